@@ -570,6 +570,113 @@ int tutti_place_classify(const void *const *planes, uint32_t n, uint64_t plane_b
 int tutti_place_pairs(const int32_t *classes, uint32_t n, uint32_t n_pairs, uint32_t strict, uint32_t *pairs,
                       uint32_t *n_mixed);
 
+/* ---- the paged cache in use: appending to the blocks that the calls above move, and attention over them.  Both calls take the
+ * pool as it is (either layout, any block_stride) and one record per sequence in device memory; they go with any token count
+ * per sequence, from one (decoding) to whole prompts, side by side in one call.
+ *
+ * Types.  `dtype` is the type of queries, keys, values and outputs.  pool->elt_bytes == 2: the blocks hold that type, and
+ * `scales` is NULL.  pool->elt_bytes == 1: the blocks hold e4m3 values (1 sign, 4 exponent, 3 mantissa bits, no infinities,
+ * largest 448) and `scales` one 32-bit factor for each block, KV head and plane: a cached value is code * scale.
+ * head_dim is a multiple of 16 and at most 128 (else TUTTI_EINVAL). */
+#define TUTTI_BF16 1u
+#define TUTTI_FP16 2u
+#define TUTTI_ST_BAD_POS 32u /* tutti_kv_append: a position that the table of angles does not have: token skipped */
+
+/* One sequence of a step: its new tokens are rows [row0, row0 + n_new) of q, k, v and out, and the last n_new of the n_held
+ * tokens that it has in the cache once they are appended; token p lies in pool block d_block_table[table_off + p / T], slot
+ * p % T.  16 bytes, device memory. */
+typedef struct tutti_seq {
+  uint32_t row0;
+  uint32_t n_new;
+  uint32_t n_held;
+  uint32_t table_off;
+} tutti_seq;
+
+/* A step's sequences (host record, device arrays).  max_new: no sequence has more new tokens than this.  n_rows: rows of q, k,
+ * v and out; the sequences' n_new add up to at most that.  Skipped with TUTTI_ST_BAD_EXTENT, nothing of theirs written: a
+ * sequence with n_new > max_new, n_new > n_held, row0 + n_new > n_rows or 2^31 tokens and more, and what is beyond n_rows where
+ * the n_new add up to more (then which part of the sequences is skipped is not said). */
+typedef struct tutti_batch {
+  const tutti_seq *d_seqs;
+  const uint32_t *d_block_table;
+  uint32_t n_seq;     /* at most TUTTI_MAX_REQ */
+  uint32_t max_new;
+  uint32_t table_len;
+  uint32_t n_rows;
+} tutti_batch;
+
+/* Rows of vectors: head i of row r begins at base + r*row_stride + i*head_stride (bytes; base and strides multiples of 16). */
+typedef struct tutti_rows {
+  void *base;
+  uint64_t row_stride;
+  uint64_t head_stride;
+} tutti_rows;
+
+/* Scales of an 8-bit pool: that of KV head i of block b is k[b*stride + i] (v[...] for values); stride >= num_kv_heads.
+ * With rows of 16 bytes (stride a multiple of 4) the scale planes are a pool of their own, blocks of stride*4 bytes, that the
+ * calls above save and restore beside the codes. */
+typedef struct tutti_scales {
+  float *k;
+  float *v;
+  uint64_t stride; /* floats */
+} tutti_scales;
+
+/* Rotation of queries and keys by their positions.  Pair j < rot_dim/2 of a head is (x[j], x[rot_dim/2 + j]), or (x[2j], x[2j+1])
+ * if interleaved; it becomes (a*c - b*s, b*c + a*s), each product and each sum rounded in 32 bits, with
+ * c = d_cos_sin[pos*rot_dim + j], s = d_cos_sin[pos*rot_dim + rot_dim/2 + j].  Values from rot_dim on stay as they are.
+ * d_pos NULL: pos is the token's place in its sequence.  Else up to four axes (time, height, width, ...): the first
+ * axis_pairs[0] pairs take pos = d_pos[row], the next axis_pairs[1] pairs d_pos[pos_stride + row], and so on; axis_pairs adds
+ * up to rot_dim/2.  A token with a position >= n_pos is skipped (TUTTI_ST_BAD_POS): its q_out row is not written and its slot
+ * in the cache keeps its bytes. */
+typedef struct tutti_rope {
+  const float *d_cos_sin; /* [n_pos][rot_dim], 16-byte aligned: rot_dim/2 cosines, then as many sines */
+  const uint32_t *d_pos;
+  uint64_t pos_stride;    /* elements from one axis to the next */
+  uint32_t n_pos;
+  uint32_t rot_dim;       /* even, at most head_dim */
+  uint32_t interleaved;
+  uint32_t axis_pairs[4];
+} tutti_rope;
+
+/* New tokens into the cache, in ONE launch: q_out <- rotated q (q == NULL: none; q_out may be q), pool slots <- rotated k, and v.
+ * rope NULL: nothing is rotated.  Tokens whose block is not in the table (BAD_BLOCK) are skipped; q_out is written all the same.
+ * 16-bit pool: every value is rounded once, to dtype.
+ * 8-bit pool, for each block and KV head that gets tokens: scale <- the smallest power of two, at least 2^-64, with
+ * |x| <= 448*scale for all finite values x that the block gets, and no less than the scale it has if it holds older tokens of
+ * the sequence (slots in front of the new ones); codes are rounded to nearest even, infinities become +-448 and a NaN stays
+ * one.  Where an older token's scale grows its codes become e4m3(code * old scale / new scale): exact, powers of two
+ * apart, but for values that fall below 2^-6 new scales.  A block whose slot 0 is among the new tokens starts afresh, whatever
+ * lies in it; slots behind the last token keep their bytes.
+ * Two sequences of one call must not append to the same block, and no block is appended to by two calls at once. */
+int tutti_kv_append(const tutti_pool *pool, const tutti_scales *scales, const tutti_batch *batch, const tutti_rope *rope,
+                    const tutti_rows *q, const tutti_rows *q_out, const tutti_rows *k, const tutti_rows *v,
+                    uint32_t n_q_heads, uint32_t dtype, uint32_t *d_status, void *stream);
+
+/* How queries attend.  Query i of a sequence, at place p = n_held - n_new + i, sees key j if j < n_held, and j <= p if causal,
+ * and j > p - window if window > 0 (with causal only).  n_q_heads: a multiple of num_kv_heads; query heads
+ * [i*g, (i+1)*g), g = n_q_heads / num_kv_heads, share KV head i. */
+typedef struct tutti_attn {
+  uint32_t n_q_heads;
+  uint32_t dtype;
+  float sm_scale;  /* finite */
+  uint32_t causal; /* 0 or 1 */
+  uint32_t window;
+} tutti_attn;
+
+/* Attention of the new tokens' queries over what their sequences hold:  s_j = sm_scale * q.k_j,  out = sum_j e^s_j v_j / sum_j e^s_j,
+ * d_lse[row*n_q_heads + head] (32 bits; may be NULL) = log sum_j e^s_j, over the keys that the query sees; a query that sees
+ * none gets out = 0 and lse = -infinity.  Keys of a block that is not in the table, or whose id is >= num_blocks, are not seen
+ * (BAD_BLOCK).  Slots that no query of the sequence sees may hold anything, NaN included.
+ * Scores, maxima, sums and products are 32-bit; the weights e^(s_j - max) are rounded to the 16-bit type that meets the values
+ * in the matrix instructions (fp16 for e4m3 values, else dtype), and the result once to dtype.  Scales are positive and finite.
+ * d_work: work_bytes >= tutti_kv_attend_work_bytes(...) bytes of device memory (16-byte aligned, contents garbage before and
+ * after) in which long sequences' parts meet; calls that may overlap need their own.  The size depends on the pool's shape,
+ * batch->n_rows, n_seq, max_new and attn alone, and 0 comes back for arguments that the call refuses. */
+uint64_t tutti_kv_attend_work_bytes(const tutti_pool *pool, const tutti_batch *batch, const tutti_attn *attn);
+int tutti_kv_attend(const tutti_pool *pool, const tutti_scales *scales, const tutti_batch *batch, const tutti_attn *attn,
+                    const tutti_rows *q, const tutti_rows *out, float *d_lse, void *d_work, uint64_t work_bytes,
+                    uint32_t *d_status, void *stream);
+
 /* ---- housekeeping */
 const char *tutti_strerror(int code);
 int tutti_last_hip_error(void);     /* hipError_t of the last failed HIP call on this thread, 0 if none */

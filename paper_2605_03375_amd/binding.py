@@ -32,7 +32,8 @@ OP_READ, OP_WRITE = 1, 2
 STREAM_SLOTS = 4096
 IOCB_SLOTS = 2048
 MAX_REQ = 2048
-ST_BAD_BLOCK, ST_STAGE_CAP, ST_SQE_CAP, ST_DUP_BLOCK, ST_BAD_EXTENT = 1, 2, 4, 8, 16
+ST_BAD_BLOCK, ST_STAGE_CAP, ST_SQE_CAP, ST_DUP_BLOCK, ST_BAD_EXTENT, ST_BAD_POS = 1, 2, 4, 8, 16, 32
+BF16, FP16 = 1, 2   # types of queries, keys, values and outputs
 
 # Declarations of the C records for decoding results on the host.
 EXTENT_DTYPE = np.dtype({"names": ["stage_off", "obj_bytes", "n_blocks", "n_chunks", "sqe_base", "table_off"],
@@ -59,7 +60,8 @@ EXPORTS = ["tutti_obj_layout", "tutti_obj_pack", "tutti_obj_unpack", "tutti_sqe_
            "tutti_table_order_work_bytes", "tutti_retrieve_layer_issue", "tutti_store_layer_issue",
            "tutti_complete_io", "tutti_wait_cqe_range", "tutti_place_work_bytes", "tutti_place_pair_times",
            "tutti_place_classify", "tutti_place_pairs", "tutti_retrieve_layer_chained",
-           "tutti_store_layer_chained", "tutti_issue_io_chained"]
+           "tutti_store_layer_chained", "tutti_issue_io_chained", "tutti_kv_append", "tutti_kv_attend",
+           "tutti_kv_attend_work_bytes"]
 BENCH_EXPORTS = ["tutti_copy_baseline", "tutti_stream_baseline", "tutti_scatter_baseline", "tutti_set_tuning",
                  "tutti_set_nontemporal", "tutti_set_hnd_mode", "tutti_set_xcd_mapping",
                  "tutti_host_cost_of_restore"]   # include/tutti_bench.h
@@ -84,6 +86,32 @@ class tutti_ring(C.Structure):
 class tutti_filestore(C.Structure):
     _fields_ = [("base", C.c_void_p), ("file_stride", C.c_uint64), ("first_file_id", C.c_uint32),
                 ("n_files", C.c_uint32)]
+
+
+class tutti_batch(C.Structure):
+    _fields_ = [("d_seqs", C.c_void_p), ("d_block_table", C.c_void_p), ("n_seq", C.c_uint32), ("max_new", C.c_uint32),
+                ("table_len", C.c_uint32), ("n_rows", C.c_uint32)]
+
+
+class tutti_rows(C.Structure):
+    _fields_ = [("base", C.c_void_p), ("row_stride", C.c_uint64), ("head_stride", C.c_uint64)]
+
+
+class tutti_scales(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("stride", C.c_uint64)]
+
+
+class tutti_rope(C.Structure):
+    _fields_ = [("d_cos_sin", C.c_void_p), ("d_pos", C.c_void_p), ("pos_stride", C.c_uint64), ("n_pos", C.c_uint32),
+                ("rot_dim", C.c_uint32), ("interleaved", C.c_uint32), ("axis_pairs", C.c_uint32 * 4)]
+
+
+class tutti_attn(C.Structure):
+    _fields_ = [("n_q_heads", C.c_uint32), ("dtype", C.c_uint32), ("sm_scale", C.c_float), ("causal", C.c_uint32),
+                ("window", C.c_uint32)]
+
+
+SEQ_DTYPE = np.dtype([("row0", "<u4"), ("n_new", "<u4"), ("n_held", "<u4"), ("table_off", "<u4")])
 
 
 class tutti_sq_state(C.Structure):
@@ -175,6 +203,11 @@ def _declare(L, bench):
     L.tutti_store_layer_chained.argtypes = L.tutti_retrieve_layer_chained.argtypes
     L.tutti_sgl_table_build.argtypes = [pp, u64, u64, u32, vp, u32, vp, vp]
     L.tutti_sqe_build_direct.argtypes = [pp, pc, vp, u32, vp, u32, vp, u32, u32, u64, u32, vp, u32, vp, vp]
+    pb, prows, psc = C.POINTER(tutti_batch), C.POINTER(tutti_rows), C.POINTER(tutti_scales)
+    L.tutti_kv_append.argtypes = [pp, psc, pb, C.POINTER(tutti_rope), prows, prows, prows, prows, u32, u32, vp, vp]
+    L.tutti_kv_attend.argtypes = [pp, psc, pb, C.POINTER(tutti_attn), prows, prows, vp, vp, u64, vp, vp]
+    L.tutti_kv_attend_work_bytes.argtypes = [pp, pb, C.POINTER(tutti_attn)]
+    L.tutti_kv_attend_work_bytes.restype = u64
     L.tutti_strerror.argtypes = [C.c_int]
     L.tutti_strerror.restype = C.c_char_p
     L.tutti_version.restype = u32
@@ -200,7 +233,7 @@ def _declare(L, bench):
     L.tutti_place_pairs.argtypes = [C.POINTER(C.c_int32), u32, u32, u32, C.POINTER(u32), C.POINTER(u32)]
     for name in EXPORTS:
         if name not in ("tutti_strerror", "tutti_version", "tutti_sq_free_count", "tutti_table_validate_work_bytes",
-                        "tutti_table_order_work_bytes", "tutti_place_work_bytes"):
+                        "tutti_table_order_work_bytes", "tutti_place_work_bytes", "tutti_kv_attend_work_bytes"):
             getattr(L, name).restype = C.c_int
     if bench:
         L.tutti_copy_baseline.argtypes = [vp, vp, u64, u32, vp]
@@ -312,6 +345,54 @@ def make_pool(k_base, v_base, *, num_blocks, block_tokens, num_kv_heads, head_di
     p.head_dim, p.elt_bytes, p.pool_layout = head_dim, elt_bytes, pool_layout
     p._keep = (k_base, v_base)
     return p
+
+
+def make_batch(d_seqs, n_seq, max_new, d_block_table, table_len, n_rows):
+    """A step's sequences: records of SEQ_DTYPE and block ids in device memory, and what bounds them."""
+    b = tutti_batch(_p(d_seqs), _p(d_block_table), n_seq, max_new, table_len, n_rows)
+    b._keep = (d_seqs, d_block_table)
+    return b
+
+
+def make_rows(rows, row_stride=None, head_stride=None):
+    """Rows of vectors: a tensor [rows, heads, head size] whose heads are contiguous, or a pointer and byte strides."""
+    if row_stride is None:
+        if rows.dim() != 3 or (rows.shape[2] > 1 and rows.stride(2) != 1):
+            raise ValueError("rows: a tensor [rows, heads, head size] with contiguous heads")
+        size = rows.element_size()
+        row_stride, head_stride = rows.stride(0) * size, rows.stride(1) * size
+    r = tutti_rows(_p(rows), row_stride, head_stride)
+    r._keep = rows
+    return r
+
+
+def make_scales(k, v, stride=None):
+    """Scales of an 8-bit pool: two tensors [blocks, floats of a row] of 32-bit floats, or pointers and the floats of a row."""
+    if stride is None:
+        if k.shape != v.shape or k.stride() != v.stride() or k.stride(1) != 1 or k.element_size() != 4:
+            raise ValueError("scales: two tensors [blocks, KV heads or more] of 32-bit floats, alike")
+        stride = k.stride(0)
+    s = tutti_scales(_p(k), _p(v), stride)
+    s._keep = (k, v)
+    return s
+
+
+def make_rope(d_cos_sin, rot_dim, n_pos=None, d_pos=None, pos_stride=None, pairs=None, interleaved=False):
+    """Rotation by positions: d_cos_sin [positions, rot_dim]; d_pos [axes, rows] with `pairs` pairs of each axis, or None: a
+    token's place in its sequence."""
+    r = tutti_rope()
+    r.d_cos_sin, r.d_pos, r.rot_dim, r.interleaved = _p(d_cos_sin), _p(d_pos), rot_dim, 1 if interleaved else 0
+    r.n_pos = d_cos_sin.shape[0] if n_pos is None else n_pos
+    if d_pos is not None:
+        r.pos_stride = d_pos.stride(0) if pos_stride is None else pos_stride
+    for i, n in enumerate((rot_dim // 2,) if pairs is None else pairs):
+        r.axis_pairs[i] = n
+    r._keep = (d_cos_sin, d_pos)
+    return r
+
+
+def make_attn(n_q_heads, dtype, sm_scale, causal=True, window=0):
+    return tutti_attn(n_q_heads, dtype, sm_scale, 1 if causal else 0, window)
 
 
 def make_cfg(align=4096, chunk_bytes=2 << 20, num_layers=1):
@@ -699,6 +780,28 @@ def tutti_place_pairs(classes, n_pairs, strict=True):
     n_mixed = C.c_uint32(0)
     _check("tutti_place_pairs", lib().tutti_place_pairs(cls, n, n_pairs, 1 if strict else 0, pairs, C.byref(n_mixed)))
     return [(pairs[2 * i], pairs[2 * i + 1]) for i in range(n_pairs)], n_mixed.value
+
+
+def _ref(record):
+    return None if record is None else C.byref(record)
+
+
+def tutti_kv_append(pool, scales, batch, rope, q, q_out, k, v, n_q_heads, dtype, d_status=None, stream=None):
+    """New tokens' keys (rotated) and values into the paged cache, rotated queries to q_out."""
+    return _check("tutti_kv_append", lib().tutti_kv_append(_ref(pool), _ref(scales), _ref(batch), _ref(rope), _ref(q),
+                                                           _ref(q_out), _ref(k), _ref(v), n_q_heads, dtype, _p(d_status),
+                                                           _stream(stream)))
+
+
+def tutti_kv_attend_work_bytes(pool, batch, attn):
+    return lib().tutti_kv_attend_work_bytes(_ref(pool), _ref(batch), _ref(attn))
+
+
+def tutti_kv_attend(pool, scales, batch, attn, q, out, d_lse, d_work, work_bytes, d_status=None, stream=None):
+    """Attention of the new tokens' queries over what their sequences hold in the paged cache."""
+    return _check("tutti_kv_attend", lib().tutti_kv_attend(_ref(pool), _ref(scales), _ref(batch), _ref(attn), _ref(q),
+                                                           _ref(out), _p(d_lse), _p(d_work), work_bytes, _p(d_status),
+                                                           _stream(stream)))
 
 
 def tutti_host_cost_of_restore(pool, cfg, d_n_blocks, n_req, d_block_table, table_len, d_file_id, layer, d_stage,

@@ -18,9 +18,11 @@ BENCH_LIB = os.path.join(HERE, "libtutti_bench.so")  # the same sources with the
 # Python callables of the per-layer entry points (host code only); the name says which Python it is for
 FAST_CALL = os.path.join(HERE, "_fast_call" + sysconfig.get_config_var("EXT_SUFFIX"))
 FAST_CALL_DEPS = [os.path.join(CSRC, "fast_call.cpp"), os.path.join(ROOT, "include", "tutti.h")]
-SOURCES = [os.path.join(CSRC, "tutti_api.hip"), os.path.join(CSRC, "tutti_host.cpp")]
+SOURCES = [os.path.join(CSRC, "tutti_api.hip"), os.path.join(CSRC, "tutti_host.cpp"), os.path.join(CSRC, "kv_api.hip")]
 DEPS = SOURCES + [os.path.join(CSRC, "tutti_kernels.hip.h"), os.path.join(CSRC, "launch_rules.h"),
-                  os.path.join(CSRC, "layer_call.h"),
+                  os.path.join(CSRC, "layer_call.h"), os.path.join(CSRC, "library_state.h"),
+                  os.path.join(CSRC, "kv_common.hip.h"), os.path.join(CSRC, "kv_append.hip.h"),
+                  os.path.join(CSRC, "kv_attend.hip.h"),
                   os.path.join(ROOT, "include", "tutti.h"),
                   os.path.join(ROOT, "include", "tutti_bench.h")]
 

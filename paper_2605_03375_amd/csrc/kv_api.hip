@@ -1,0 +1,266 @@
+// Host side of the calls that use a paged cache in place: tutti_kv_append, tutti_kv_attend.  As everywhere in the library a call
+// checks its host arguments in O(1), enqueues a constant number of kernels on the caller's stream and returns.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "kv_append.hip.h"
+#include "kv_attend.hip.h"
+#include "library_state.h"
+#include "tutti.h"
+
+namespace {
+
+using namespace tutti;
+
+bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+int check_pool(const tutti_pool *pool, const tutti_scales *scales, uint32_t dtype) {
+  if (!pool) return TUTTI_EINVAL;
+  if (dtype != TUTTI_BF16 && dtype != TUTTI_FP16) return TUTTI_EINVAL;
+  if (pool->elt_bytes != 1 && pool->elt_bytes != 2) return TUTTI_EINVAL;
+  if (pool->head_dim == 0 || pool->head_dim % 16 != 0 || pool->head_dim > 128) return TUTTI_EINVAL;
+  if (pool->num_blocks == 0 || pool->block_tokens == 0 || pool->num_kv_heads == 0) return TUTTI_EINVAL;
+  if (pool->pool_layout != TUTTI_LAYOUT_NHD && pool->pool_layout != TUTTI_LAYOUT_HND) return TUTTI_EINVAL;
+  uint64_t b = static_cast<uint64_t>(pool->block_tokens) * pool->num_kv_heads;
+  if (b > 0xffffffffull) return TUTTI_EINVAL;
+  b *= pool->head_dim * pool->elt_bytes;  // (at most 256)
+  if (b > 0xffffffffull || pool->block_stride < b || pool->block_stride % 16 != 0) return TUTTI_EINVAL;
+  if (!pool->k_base || !pool->v_base || !aligned(pool->k_base, 16) || !aligned(pool->v_base, 16)) return TUTTI_EINVAL;
+  if ((pool->elt_bytes == 1) != (scales != nullptr)) return TUTTI_EINVAL;
+  if (scales && (!scales->k || !scales->v || !aligned(scales->k, 4) || !aligned(scales->v, 4) ||
+                 scales->stride < pool->num_kv_heads))
+    return TUTTI_EINVAL;
+  return TUTTI_OK;
+}
+
+int check_batch(const tutti_batch *b) {
+  if (!b) return TUTTI_EINVAL;
+  if (b->n_seq > TUTTI_MAX_REQ || b->n_rows >= 0x80000000u) return TUTTI_ERANGE;
+  if (b->n_seq == 0 || b->n_rows == 0 || b->max_new == 0) return TUTTI_OK;
+  if (!b->d_seqs || !aligned(b->d_seqs, 16)) return TUTTI_EINVAL;
+  if (b->table_len && (!b->d_block_table || !aligned(b->d_block_table, 4))) return TUTTI_EINVAL;
+  return TUTTI_OK;
+}
+bool nothing_to_do(const tutti_batch *b) { return b->n_seq == 0 || b->n_rows == 0 || b->max_new == 0; }
+
+bool good_rows(const tutti_rows *r) {
+  return r && r->base && aligned(r->base, 16) && r->row_stride % 16 == 0 && r->head_stride % 16 == 0;
+}
+
+PoolView view(const tutti_pool *p, const tutti_scales *s) {
+  PoolView v{};
+  v.k = static_cast<uint8_t *>(p->k_base);
+  v.v = static_cast<uint8_t *>(p->v_base);
+  v.block_stride = p->block_stride;
+  const uint32_t row = p->head_dim * p->elt_bytes;
+  const bool hnd = p->pool_layout == TUTTI_LAYOUT_HND;
+  v.token_stride = hnd ? row : row * p->num_kv_heads;
+  v.head_stride = hnd ? row * p->block_tokens : row;
+  v.num_blocks = p->num_blocks;
+  v.block_tokens = p->block_tokens;
+  v.shift = 255;
+  for (uint32_t i = 0; i < 32; ++i)
+    if (p->block_tokens == 1u << i) v.shift = i;
+  if (s) {
+    v.k_scale = s->k;
+    v.v_scale = s->v;
+    v.scale_stride = s->stride;
+  }
+  return v;
+}
+
+BatchView view(const tutti_batch *b) {
+  return BatchView{b->d_seqs, b->d_block_table, b->n_seq, b->max_new, b->table_len, b->n_rows};
+}
+
+int launched() {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? TUTTI_OK : hip_failed(e);
+}
+
+// ---- append
+
+template <typename T, bool E4M3>
+void launch_append(const AppendArgs &a, uint32_t grid, hipStream_t stream) {
+  if (a.d <= 64)
+    hipLaunchKernelGGL((k_kv_append<T, E4M3, 8>), dim3(grid), dim3(256), 0, stream, a);
+  else
+    hipLaunchKernelGGL((k_kv_append<T, E4M3, 16>), dim3(grid), dim3(256), 0, stream, a);
+}
+
+// ---- attend
+
+// Rows of queries a workgroup takes: 16 where no sequence has more, else 32.
+uint32_t rows_a_tile(const tutti_batch *b, uint32_t group) {
+  return static_cast<uint64_t>(b->max_new) * group <= 16 ? 16 : 32;
+}
+
+struct AttendSizes {
+  uint32_t rows, dp, target, max_units, max_parts;
+  uint64_t ml_bytes, bytes;
+};
+
+// Parts that the keys of all sequences are split into come to at most 2 * target (a sequence is split only if it has more
+// tiles than one part takes), units to at most target + the row tiles that there can be.
+int attend_sizes(const tutti_pool *pool, const tutti_batch *b, const tutti_attn *attn, AttendSizes *s) {
+  const uint32_t group = attn->n_q_heads / pool->num_kv_heads;
+  s->rows = rows_a_tile(b, group);
+  s->dp = pool->head_dim <= 64 ? 64 : 128;
+  s->target = 1024;
+  const uint64_t tiles = static_cast<uint64_t>(b->n_rows) * group / s->rows + std::min(b->n_seq, b->n_rows);
+  const uint64_t units = s->target + tiles * pool->num_kv_heads;
+  if (units >= 0x80000000ull || static_cast<uint64_t>(b->n_rows) * attn->n_q_heads >= 0x80000000ull) return TUTTI_ERANGE;
+  s->max_units = static_cast<uint32_t>(units);
+  s->max_parts = 2 * s->target;
+  s->ml_bytes = static_cast<uint64_t>(s->max_parts) * s->rows * sizeof(f32x2);
+  s->bytes = s->ml_bytes + static_cast<uint64_t>(s->max_parts) * s->rows * s->dp * sizeof(float);
+  return TUTTI_OK;
+}
+
+int check_attn(const tutti_pool *pool, const tutti_attn *attn) {
+  if (!attn || attn->n_q_heads == 0 || attn->n_q_heads % pool->num_kv_heads != 0) return TUTTI_EINVAL;
+  if (!std::isfinite(attn->sm_scale) || attn->causal > 1 || (attn->window && !attn->causal)) return TUTTI_EINVAL;
+  return TUTTI_OK;
+}
+
+template <typename T, bool E4M3, int DP, bool PAGED16, int RT>
+void launch_attend(const AttendArgs &a, hipStream_t stream) {
+  hipLaunchKernelGGL((k_kv_attend<T, E4M3, DP, PAGED16, RT>), dim3(a.max_units), dim3(256), 0, stream, a);
+  const uint32_t joins = (a.batch.n_rows * a.kv_heads * a.group + 3) / 4;
+  hipLaunchKernelGGL((k_kv_join<T, DP, RT * 16>), dim3(joins), dim3(256), 0, stream, a);
+}
+template <typename T, bool E4M3, int DP>
+void launch_attend(const AttendArgs &a, uint32_t rows, hipStream_t stream) {
+  if (a.pool.block_tokens % 16 == 0)
+    rows == 16 ? launch_attend<T, E4M3, DP, true, 1>(a, stream) : launch_attend<T, E4M3, DP, true, 2>(a, stream);
+  else
+    rows == 16 ? launch_attend<T, E4M3, DP, false, 1>(a, stream) : launch_attend<T, E4M3, DP, false, 2>(a, stream);
+}
+template <typename T>
+void launch_attend(const AttendArgs &a, bool e4m3, uint32_t rows, hipStream_t stream) {
+  if (e4m3)
+    a.d <= 64 ? launch_attend<T, true, 64>(a, rows, stream) : launch_attend<T, true, 128>(a, rows, stream);
+  else
+    a.d <= 64 ? launch_attend<T, false, 64>(a, rows, stream) : launch_attend<T, false, 128>(a, rows, stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+int tutti_kv_append(const tutti_pool *pool, const tutti_scales *scales, const tutti_batch *batch, const tutti_rope *rope,
+                    const tutti_rows *q, const tutti_rows *q_out, const tutti_rows *k, const tutti_rows *v,
+                    uint32_t n_q_heads, uint32_t dtype, uint32_t *d_status, void *stream) {
+  int rc = check_pool(pool, scales, dtype);
+  if (rc) return rc;
+  if ((rc = check_batch(batch)) != TUTTI_OK) return rc;
+  if (!aligned(d_status, 4)) return TUTTI_EINVAL;
+  if (!good_rows(k) || !good_rows(v)) return TUTTI_EINVAL;
+  if (q && (!good_rows(q) || !good_rows(q_out) || n_q_heads == 0)) return TUTTI_EINVAL;
+  AppendArgs a{};
+  if (rope) {
+    RopeView &r = a.rope;
+    if (rope->rot_dim % 2 != 0 || rope->rot_dim == 0 || rope->rot_dim > pool->head_dim || rope->interleaved > 1) return TUTTI_EINVAL;
+    if (!rope->d_cos_sin || !aligned(rope->d_cos_sin, 16) || rope->n_pos == 0 || !aligned(rope->d_pos, 4)) return TUTTI_EINVAL;
+    r.cos_sin = rope->d_cos_sin;
+    r.pos = rope->d_pos;
+    r.pos_stride = rope->pos_stride;
+    r.n_pos = rope->n_pos;
+    r.rot = rope->rot_dim;
+    r.half = rope->rot_dim / 2;
+    r.interleaved = rope->interleaved;
+    if (rope->d_pos) {
+      uint64_t end = 0;
+      for (int i = 0; i < 4; ++i) {
+        end += rope->axis_pairs[i];
+        if (i < 3) r.end[i] = static_cast<uint32_t>(std::min<uint64_t>(end, r.half));
+        if (rope->axis_pairs[i]) r.axes |= 1u << i;
+      }
+      if (end != r.half) return TUTTI_EINVAL;
+    } else {
+      r.end[0] = r.end[1] = r.end[2] = r.half;
+      r.axes = 1;
+    }
+  }
+  if (nothing_to_do(batch)) return TUTTI_OK;
+  a.pool = view(pool, scales);
+  a.batch = view(batch);
+  if (q) {
+    a.q = *q;
+    a.q_out = *q_out;
+    a.q_heads = n_q_heads;
+  }
+  a.k = *k;
+  a.v = *v;
+  a.kv_heads = pool->num_kv_heads;
+  a.d = pool->head_dim;
+  a.status = d_status;
+  const bool e4m3 = scales != nullptr;
+  a.heads_a_job = 4;
+  a.q_jobs = (a.q_heads + a.heads_a_job - 1) / a.heads_a_job;
+  a.jobs = a.q_jobs + 2 * (e4m3 ? a.kv_heads : (a.kv_heads + a.heads_a_job - 1) / a.heads_a_job);
+  // a unit has at least one new token, and only a sequence's first and last may have fewer than a whole unit's
+  const uint64_t tokens = e4m3 ? pool->block_tokens : kLanes / (a.d <= 64 ? 8 : 16);
+  const uint64_t units = std::min<uint64_t>(batch->n_rows, batch->n_rows / tokens + 2ull * batch->n_seq);
+  if (units * a.jobs >= 0x80000000ull) return TUTTI_ERANGE;
+  a.max_units = static_cast<uint32_t>(units);
+  const uint32_t grid = static_cast<uint32_t>((units * a.jobs + 3) / 4);
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  if (dtype == TUTTI_BF16)
+    e4m3 ? launch_append<Bf16, true>(a, grid, st) : launch_append<Bf16, false>(a, grid, st);
+  else
+    e4m3 ? launch_append<Fp16, true>(a, grid, st) : launch_append<Fp16, false>(a, grid, st);
+  return launched();
+}
+
+uint64_t tutti_kv_attend_work_bytes(const tutti_pool *pool, const tutti_batch *batch, const tutti_attn *attn) {
+  AttendSizes s;
+  if (!pool || !batch || pool->num_kv_heads == 0 || check_attn(pool, attn) != TUTTI_OK) return 0;
+  if (attend_sizes(pool, batch, attn, &s) != TUTTI_OK) return 0;
+  return s.bytes;
+}
+
+int tutti_kv_attend(const tutti_pool *pool, const tutti_scales *scales, const tutti_batch *batch, const tutti_attn *attn,
+                    const tutti_rows *q, const tutti_rows *out, float *d_lse, void *d_work, uint64_t work_bytes,
+                    uint32_t *d_status, void *stream) {
+  if (!attn) return TUTTI_EINVAL;
+  int rc = check_pool(pool, scales, attn->dtype);
+  if (rc) return rc;
+  if ((rc = check_batch(batch)) != TUTTI_OK) return rc;
+  if ((rc = check_attn(pool, attn)) != TUTTI_OK) return rc;
+  if (!good_rows(q) || !good_rows(out) || !aligned(d_lse, 4) || !aligned(d_status, 4)) return TUTTI_EINVAL;
+  AttendSizes s;
+  if ((rc = attend_sizes(pool, batch, attn, &s)) != TUTTI_OK) return rc;
+  if (nothing_to_do(batch)) return TUTTI_OK;
+  if (!d_work || !aligned(d_work, 16)) return TUTTI_EINVAL;
+  if (work_bytes < s.bytes) return TUTTI_ERANGE;
+  AttendArgs a{};
+  a.pool = view(pool, scales);
+  a.batch = view(batch);
+  a.q = *q;
+  a.out = *out;
+  a.lse = d_lse;
+  a.kv_heads = pool->num_kv_heads;
+  a.group = attn->n_q_heads / pool->num_kv_heads;
+  a.d = pool->head_dim;
+  a.scale_log2 = attn->sm_scale * kLog2e;
+  a.causal = attn->causal;
+  a.window = attn->window;
+  a.target = s.target;
+  a.min_tiles = 8;
+  a.max_units = s.max_units;
+  a.max_parts = s.max_parts;
+  a.part_ml = static_cast<f32x2 *>(d_work);
+  a.part_o = reinterpret_cast<float *>(static_cast<uint8_t *>(d_work) + s.ml_bytes);
+  a.status = d_status;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  if (attn->dtype == TUTTI_BF16)
+    launch_attend<Bf16>(a, scales != nullptr, s.rows, st);
+  else
+    launch_attend<Fp16>(a, scales != nullptr, s.rows, st);
+  return launched();
+}
+
+}  // extern "C"

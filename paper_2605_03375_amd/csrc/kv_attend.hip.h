@@ -1,0 +1,625 @@
+// Attention over a paged cache: 16-bit or e4m3 blocks, any number of new tokens a sequence.
+#pragma once
+#include <type_traits>
+
+#include "kv_common.hip.h"
+
+namespace tutti {
+
+constexpr uint32_t kKeyTile = 32;    // keys that a wavefront takes at a time: two halves of 16
+constexpr uint32_t kAttendWaves = 4; // wavefronts of a workgroup: every fourth tile each
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+// A row's running maximum is raised only by steps of more than this (log2): until then its weights are at most 2^8, far from
+// the largest fp16 value, and nothing that has been summed has to be rescaled.
+constexpr float kRaise = 8.0f;
+
+struct AttendArgs {
+  PoolView pool;
+  BatchView batch;
+  tutti_rows q, out;
+  float *lse;
+  uint32_t kv_heads, group, d;  // group: query heads of one KV head
+  float scale_log2;             // sm_scale * log2(e)
+  uint32_t causal, window;
+  // How the keys are split: a sequence's tiles go in parts of about max(min_tiles, all tiles / target) tiles.
+  uint32_t target, min_tiles, max_units, max_parts;
+  float *part_o;                // [part][rows][dp]: sums of weighted values
+  f32x2 *part_ml;               // [part][rows]: running maximum (log2) and sum of weights
+  uint32_t *status;
+};
+
+// What a step's sequences come to.  Rows: new tokens times query heads of a KV head, in tiles of RT*16.
+struct Plan {
+  uint32_t tiles_a_part;
+};
+
+template <int ROWS>
+__device__ __forceinline__ uint32_t row_tiles(const AttendArgs &a, const tutti_seq &s) {
+  return (s.n_new * a.group + ROWS - 1) / ROWS;
+}
+
+// Key tiles that a sequence's queries see, counted from the tile of the first one.
+__device__ __forceinline__ uint32_t first_key(const AttendArgs &a, const tutti_seq &s) {
+  const uint32_t begin = s.n_held - s.n_new;
+  return a.window && begin + 1 > a.window ? begin + 1 - a.window : 0;
+}
+__device__ __forceinline__ uint32_t key_tiles(const AttendArgs &a, const tutti_seq &s) {
+  return (s.n_held + kKeyTile - 1) / kKeyTile - first_key(a, s) / kKeyTile;
+}
+
+template <int ROWS>
+__device__ __forceinline__ Plan make_plan(const AttendArgs &a) {
+  const uint32_t lane = threadIdx.x & (kLanes - 1);
+  uint64_t work = 0;
+  for (uint32_t base = 0; base < a.batch.n_seq; base += kLanes) {
+    if (base + lane < a.batch.n_seq) {
+      const tutti_seq s = load_seq(a.batch.seqs + base + lane);
+      if (seq_ok(a.batch, s) && s.n_new) work += static_cast<uint64_t>(row_tiles<ROWS>(a, s)) * key_tiles(a, s);
+    }
+  }
+#pragma unroll
+  for (int m = 1; m < static_cast<int>(kLanes); m <<= 1) work += __shfl_xor(work, m, kLanes);
+  work *= a.kv_heads;
+  const uint64_t each = (work + a.target - 1) / a.target;
+  Plan p;
+  p.tiles_a_part = uniform(each > 0x40000000u ? 0x40000000u : static_cast<uint32_t>(each));
+  if (p.tiles_a_part < a.min_tiles) p.tiles_a_part = a.min_tiles;
+  return p;
+}
+
+__device__ __forceinline__ uint32_t parts_of(const AttendArgs &a, const Plan &p, const tutti_seq &s) {
+  const uint32_t n = (key_tiles(a, s) + p.tiles_a_part - 1) / p.tiles_a_part;
+  return n ? n : 1;
+}
+
+// Where a unit's results go.
+struct Unit {
+  uint32_t seq;         // n_seq: none
+  tutti_seq s;
+  uint32_t row_tile, head, part, parts;
+  uint32_t part_slot;   // of its first part in the work memory, where parts > 1
+};
+
+template <int ROWS>
+__device__ __forceinline__ Unit locate(const AttendArgs &a, const Plan &p, uint32_t unit, bool first) {
+  const uint32_t lane = threadIdx.x & (kLanes - 1);
+  Unit u{};
+  u.seq = a.batch.n_seq;
+  uint32_t before = 0, slots = 0;
+  bool bad = false;
+  for (uint32_t base = 0; base < a.batch.n_seq; base += kLanes) {
+    tutti_seq s{};
+    uint32_t n = 0, split = 0, tiles = 0, parts = 0;
+    if (base + lane < a.batch.n_seq) {
+      s = load_seq(a.batch.seqs + base + lane);
+      const bool ok = seq_ok(a.batch, s);
+      bad |= !ok;
+      if (ok && s.n_new) {
+        tiles = row_tiles<ROWS>(a, s);
+        parts = parts_of(a, p, s);
+        n = tiles * a.kv_heads * parts;
+        split = parts > 1 ? n : 0;
+      }
+    }
+    const uint32_t upto = before + lane_prefix_sum(n), split_upto = slots + lane_prefix_sum(split);
+    const uint64_t behind = __ballot(n != 0 && upto > unit);
+    if (behind && u.seq == a.batch.n_seq) {
+      const uint32_t l = static_cast<uint32_t>(__builtin_ctzll(behind));
+      const uint32_t local = unit - (from_lane(upto, l) - from_lane(n, l));
+      u.seq = base + l;
+      u.s = tutti_seq{from_lane(s.row0, l), from_lane(s.n_new, l), from_lane(s.n_held, l), from_lane(s.table_off, l)};
+      u.parts = from_lane(parts, l);
+      // heads first, then parts, then row tiles: neighbours read the same blocks
+      u.head = local % a.kv_heads;
+      u.part = local / a.kv_heads % u.parts;
+      u.row_tile = local / a.kv_heads / u.parts;
+      u.part_slot = from_lane(split_upto, l) - from_lane(split, l) + (u.row_tile * a.kv_heads + u.head) * u.parts;
+      if (!first) return u;
+    }
+    before = from_lane(upto, kLanes - 1);
+    slots = from_lane(split_upto, kLanes - 1);
+  }
+  if (first) {
+    if (__ballot(bad) && lane == 0) report(a.status, TUTTI_ST_BAD_EXTENT);
+    if (before > a.max_units && lane == 0) report(a.status, TUTTI_ST_BAD_EXTENT);
+  }
+  return u;
+}
+
+template <typename T>
+__device__ __forceinline__ f32x4 product(typename T::eight a, typename T::eight b, f32x4 c) {
+  if constexpr (sizeof(typename T::one) == 2 && __is_same(T, Fp16))
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// Eight e4m3 codes as 16-bit values (exact in both types).
+template <typename T>
+__device__ __forceinline__ typename T::eight widen(u32x2 w) {
+  typename T::eight r;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    typename T::two lo, hi;
+    if constexpr (__is_same(T, Fp16)) {
+      lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[i], 1.0f, false);
+      hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[i], 1.0f, true);
+    } else {
+      lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], 1.0f, false);
+      hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], 1.0f, true);
+    }
+    r[4 * i] = lo[0];
+    r[4 * i + 1] = lo[1];
+    r[4 * i + 2] = hi[0];
+    r[4 * i + 3] = hi[1];
+  }
+  return r;
+}
+
+// Takes infinities and NaN out of a word of values; true if there were any.
+template <typename T, bool E4M3>
+__device__ __forceinline__ bool without_not_finite(uint32_t &w) {
+  const uint32_t was = w;
+  if constexpr (E4M3) {
+#pragma unroll
+    for (int i = 0; i < 32; i += 8)
+      if ((was >> i & 0x7fu) == 0x7fu) w &= ~(0xffu << i);
+  } else {
+    constexpr uint32_t e = __is_same(T, Fp16) ? 0x7c00u : 0x7f80u;
+    if ((was & e) == e) w &= 0xffff0000u;
+    if ((was >> 16 & e) == e) w &= 0xffffu;
+  }
+  return w != was;
+}
+
+// Value i of a row in the cache, as it lies there.
+template <typename T, bool E4M3>
+__device__ __forceinline__ float element(const uint8_t *row, uint32_t i) {
+  if constexpr (E4M3)
+    return (row[i] & 0x7fu) == 0x7fu ? __builtin_nanf("") : 0.0f;  // (all that is asked of it)
+  else
+    return static_cast<float>(reinterpret_cast<const typename T::one *>(row)[i]);
+}
+
+template <int N>
+struct Words;
+template <>
+struct Words<1> { using type = uint32_t; };
+template <>
+struct Words<2> { using type = u32x2; };
+template <>
+struct Words<4> { using type = u32x4; };
+template <int N>
+__device__ __forceinline__ uint32_t word(const typename Words<N>::type &w, int i) {
+  if constexpr (N == 1)
+    return w;
+  else
+    return w[i];
+}
+
+template <int N>
+__device__ __forceinline__ void set_word(typename Words<N>::type &w, int i, uint32_t x) {
+  if constexpr (N == 1)
+    w = x;
+  else
+    w[i] = x;
+}
+
+// ---- Few or many queries, one workgroup of four wavefronts to a (row tile, KV head, part of the keys).
+//
+// Scores are computed transposed, S^T = K Q^T, with 16x16x32 matrix instructions: lane (r = l % 16, g = l / 16) holds row r of
+// the queries and keys 4g..4g+3 of each half tile, which is how O^T = V^T P^T takes P, so weights stay in the lane that
+// made them.  The contraction's order is free: a lane loads 16 consecutive bytes of a key's row, and the queries are laid out to
+// match.  Of the values, a lane takes DP/16 consecutive ones of its eight keys, and puts pairs of keys together by byte
+// permutations; so nothing passes through LDS and no wavefront waits for another until the end, where the four join.
+template <typename T, bool E4M3, int DP, bool PAGED16, int RT>
+__global__ __launch_bounds__(256, 2) void k_kv_attend(const AttendArgs a) {
+  constexpr int ROWS = RT * 16, N = DP / 16;
+  constexpr int KW = E4M3 ? DP / 64 : DP / 32;       // 16-byte loads of a key a lane does
+  constexpr int VW = E4M3 ? N / 4 : N / 2;           // words of a value row a lane takes
+  constexpr uint32_t EB = E4M3 ? 1 : 2;
+  using P = std::conditional_t<E4M3, Fp16, T>;
+  using VWords = typename Words<VW>::type;
+
+  const uint32_t lane = threadIdx.x & (kLanes - 1), wave = uniform(threadIdx.x / kLanes);
+  const uint32_t r = lane & 15u, g = lane >> 4;
+  const bool reporter = blockIdx.x == 0 && wave == 0;
+  if (blockIdx.x >= a.max_units) return;
+  const Plan plan = make_plan<ROWS>(a);
+  const Unit u = locate<ROWS>(a, plan, blockIdx.x, reporter);
+  if (u.seq == a.batch.n_seq) return;
+  if (u.parts > 1 && u.part_slot + u.parts > a.max_parts) {
+    if (threadIdx.x == 0) report(a.status, TUTTI_ST_BAD_EXTENT);
+    return;
+  }
+  const tutti_seq s = u.s;
+  const uint32_t begin = s.n_held - s.n_new, n_rows = s.n_new * a.group;
+
+  // the keys that this lane's rows see: [lo, hi)
+  uint32_t lo[RT], hi[RT];
+  const uint8_t *q_at[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const uint32_t row = u.row_tile * ROWS + t * 16 + r;
+    const uint32_t i = row < n_rows ? row / a.group : 0, head = u.head * a.group + (row < n_rows ? row - i * a.group : 0);
+    const uint32_t place = begin + i;
+    hi[t] = a.causal ? place + 1 : s.n_held;
+    lo[t] = a.window && place + 1 > a.window ? place + 1 - a.window : 0;
+    q_at[t] = static_cast<const uint8_t *>(a.q.base) + static_cast<uint64_t>(s.row0 + i) * a.q.row_stride + head * a.q.head_stride;
+  }
+  // those that any row of the tile sees, and those that all of them see
+  const uint32_t row_a = u.row_tile * ROWS, row_b = min(row_a + ROWS, n_rows) - 1;
+  const uint32_t place_a = begin + row_a / a.group, place_b = begin + row_b / a.group;
+  const uint32_t any_hi = uniform(a.causal ? place_b + 1 : s.n_held), all_hi = uniform(a.causal ? place_a + 1 : s.n_held);
+  const uint32_t any_lo = uniform(a.window && place_a + 1 > a.window ? place_a + 1 - a.window : 0);
+  const uint32_t all_lo = uniform(a.window && place_b + 1 > a.window ? place_b + 1 - a.window : 0);
+  const uint32_t tile_lo = any_lo / kKeyTile, tile_hi = (any_hi + kKeyTile - 1) / kKeyTile;
+  const uint32_t tiles = tile_hi - tile_lo;
+  const uint32_t t0 = uniform(tile_lo + static_cast<uint32_t>(static_cast<uint64_t>(tiles) * u.part / u.parts));
+  const uint32_t t1 = uniform(tile_lo + static_cast<uint32_t>(static_cast<uint64_t>(tiles) * (u.part + 1) / u.parts));
+
+  // queries, in the order of the contraction that the keys' loads give
+  typename T::eight q[RT][DP / 32];
+#pragma unroll
+  for (int t = 0; t < RT; ++t)
+#pragma unroll
+    for (int j = 0; j < DP / 32; ++j) {
+      const uint32_t e = E4M3 ? (j / 2) * 64 + g * 16 + (j & 1) * 8 : j * 32 + g * 8;
+      u32x4 w = {0, 0, 0, 0};
+      if (e < a.d) w = *reinterpret_cast<const u32x4 *>(q_at[t] + 2 * e);
+      q[t][j] = __builtin_bit_cast(typename T::eight, w);
+    }
+
+  f32x4 o[RT][N];
+  float m[RT], l[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    m[t] = kLowest;
+    l[t] = 0.0f;
+#pragma unroll
+    for (int n = 0; n < N; ++n) o[t][n] = f32x4{0, 0, 0, 0};
+  }
+
+  const uint64_t head_at = static_cast<uint64_t>(u.head) * a.pool.head_stride;
+  const uint32_t ts = a.pool.token_stride;
+  bool skipped = false;
+  for (uint32_t tile = t0 + wave; tile < t1; tile += kAttendWaves) {
+    const uint32_t key0 = tile * kKeyTile;
+    // the blocks: of each half tile (PAGED16: a half lies in one block), or of each key
+    float ck[2][4], cv[2][4], iv[2][4];              // factor of the scores, log2 and reciprocal of the values' scale
+    bool there[2][4];
+    const uint8_t *k_at[2], *v_at[2][4];
+    bool edge = key0 < all_lo || key0 + kKeyTile > all_hi;
+    if constexpr (PAGED16) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t key = key0 + 16 * h;
+        const uint32_t n = block_of(a.pool, key);
+        const uint64_t at = static_cast<uint64_t>(s.table_off) + n;
+        uint32_t id = 0;
+        bool ok = key + 16 > any_lo && key < any_hi;
+        if (ok) {
+          ok = at < a.batch.table_len;
+          if (ok) {
+            id = constant(a.batch.table)[at];
+            ok = id < a.pool.num_blocks;
+            id = ok ? id : 0;
+          }
+          if (!ok) skipped = true;
+        }
+        if (!ok) edge = true;
+        const uint64_t off = id * a.pool.block_stride + head_at + static_cast<uint64_t>(key - n * a.pool.block_tokens) * ts;
+        k_at[h] = a.pool.k + off + r * ts;
+        float f = a.scale_log2, lg = 0.0f, rc = 1.0f;
+        if constexpr (E4M3) {
+          f *= constant(a.pool.k_scale)[id * a.pool.scale_stride + u.head];
+          const float sv = constant(a.pool.v_scale)[id * a.pool.scale_stride + u.head];
+          lg = __builtin_amdgcn_logf(sv);
+          rc = ok ? 1.0f / sv : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v_at[h][i] = a.pool.v + off + (4 * g + i) * ts;
+          ck[h][i] = f;
+          cv[h][i] = lg;
+          iv[h][i] = rc;
+          there[h][i] = ok;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        // lane r looks up key r of the half; the others' come from it
+        const uint32_t key = key0 + 16 * h + r;
+        const uint32_t n = block_of(a.pool, key);
+        const uint64_t at = static_cast<uint64_t>(s.table_off) + n;
+        uint32_t id = 0;
+        bool ok = key >= any_lo && key < any_hi;
+        if (ok) {
+          ok = at < a.batch.table_len;
+          if (ok) {
+            id = a.batch.table[at];
+            ok = id < a.pool.num_blocks;
+            id = ok ? id : 0;
+          }
+          if (!ok) skipped = true;
+        }
+        if (__ballot(!ok)) edge = true;
+        const uint32_t slot = ok ? key - n * a.pool.block_tokens : 0;
+        k_at[h] = a.pool.k + id * a.pool.block_stride + head_at + static_cast<uint64_t>(slot) * ts;
+        float f = a.scale_log2, lg = 0.0f, rc = 1.0f;
+        if constexpr (E4M3) {
+          f *= a.pool.k_scale[id * a.pool.scale_stride + u.head];
+          const float sv = a.pool.v_scale[id * a.pool.scale_stride + u.head];
+          lg = __builtin_amdgcn_logf(sv);
+          rc = ok ? 1.0f / sv : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int from = static_cast<int>(4 * g + i);
+          const uint32_t id_i = __shfl(id, from, 16), slot_i = __shfl(slot, from, 16);
+          v_at[h][i] = a.pool.v + id_i * a.pool.block_stride + head_at + static_cast<uint64_t>(slot_i) * ts;
+          ck[h][i] = __shfl(f, from, 16);
+          cv[h][i] = __shfl(lg, from, 16);
+          iv[h][i] = __shfl(rc, from, 16);
+          there[h][i] = __shfl(static_cast<int>(ok), from, 16);
+        }
+      }
+    }
+    u32x4 kw[2][KW];
+    VWords vw[8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int j = 0; j < KW; ++j) {
+        kw[h][j] = u32x4{0, 0, 0, 0};
+        if (j * 64 + g * 16 < a.d * EB) kw[h][j] = *reinterpret_cast<const u32x4 *>(k_at[h] + j * 64 + g * 16);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        vw[4 * h + i] = VWords{};
+        if (r * (VW * 4) < a.d * EB) vw[4 * h + i] = *reinterpret_cast<const VWords *>(v_at[h][i] + r * (VW * 4));
+      }
+    }
+    // values of keys that no row sees are whatever lies there: nothing of them may reach a product, not even times 0
+    if (edge) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t key = key0 + 16 * h + 4 * g + i;
+          if (!there[h][i] || key < any_lo || key >= any_hi) vw[4 * h + i] = VWords{};
+        }
+    }
+    typename P::eight p[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      f32x4 sc[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        sc[h] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < KW; ++j) {
+          if constexpr (E4M3) {
+            sc[h] = product<T>(widen<T>(u32x2{kw[h][j][0], kw[h][j][1]}), q[t][2 * j], sc[h]);
+            sc[h] = product<T>(widen<T>(u32x2{kw[h][j][2], kw[h][j][3]}), q[t][2 * j + 1], sc[h]);
+          } else {
+            sc[h] = product<T>(__builtin_bit_cast(typename T::eight, kw[h][j]), q[t][j], sc[h]);
+          }
+        }
+      }
+      float x[8];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[4 * h + i] = sc[h][i] * ck[h][i] + cv[h][i];
+      if (edge) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t key = key0 + 16 * h + 4 * g + i;
+            if (!there[h][i] || key < lo[t] || key >= hi[t]) x[4 * h + i] = -__builtin_inff();
+          }
+      }
+      float top = x[0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i]);
+      top = max_over_rows(top);
+      if (__ballot(top > m[t] + kRaise)) {
+        const float raised = top > m[t] + kRaise ? top : m[t];
+        const float by = __builtin_amdgcn_exp2f(m[t] - raised);
+        m[t] = raised;
+        l[t] *= by;
+#pragma unroll
+        for (int n = 0; n < N; ++n) o[t][n] *= by;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float w = __builtin_amdgcn_exp2f(x[i] - m[t]);
+        l[t] += E4M3 ? w * iv[i / 4][i % 4] : w;
+        p[t][i] = static_cast<typename P::one>(w);
+      }
+    }
+    // an infinity or NaN that some rows see and others do not: 0 times it is not 0.  It stays out of the products and is
+    // added to the rows that see it (its weight is positive, so what it adds is itself)
+    bool odd = false;
+    if (edge) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int c = 0; c < VW; ++c) {
+          uint32_t w = word<VW>(vw[i], c);
+          odd |= without_not_finite<T, E4M3>(w);
+          set_word<VW>(vw[i], c, w);
+        }
+      odd = __ballot(odd) != 0;
+    }
+    // O^T += V^T P^T, 16 values at a time: value n of the lane's, of its eight keys
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      u32x4 w;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const uint32_t x = word<VW>(vw[2 * c], E4M3 ? n / 4 : n / 2), y = word<VW>(vw[2 * c + 1], E4M3 ? n / 4 : n / 2);
+        if constexpr (E4M3) {
+          const uint32_t pair = __builtin_amdgcn_perm(y, x, (n & 2) ? 0x07030602u : 0x05010400u);
+          const f16x2 two = (n & 1) ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(pair, 1.0f, true)
+                                    : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(pair, 1.0f, false);
+          w[c] = __builtin_bit_cast(uint32_t, two);
+        } else {
+          w[c] = __builtin_amdgcn_perm(y, x, (n & 1) ? 0x07060302u : 0x05040100u);
+        }
+      }
+      const typename P::eight v = __builtin_bit_cast(typename P::eight, w);
+#pragma unroll
+      for (int t = 0; t < RT; ++t) o[t][n] = product<P>(v, p[t], o[t][n]);
+    }
+    if (odd) {
+      for (uint32_t key = max(key0, any_lo); key < min(key0 + kKeyTile, any_hi); ++key) {
+        const uint32_t n = block_of(a.pool, key);
+        const uint64_t at = static_cast<uint64_t>(s.table_off) + n;
+        const uint32_t id = at < a.batch.table_len ? a.batch.table[at] : ~0u;
+        if (id >= a.pool.num_blocks) continue;
+        const uint8_t *row = a.pool.v + id * a.pool.block_stride + head_at + static_cast<uint64_t>(key - n * a.pool.block_tokens) * ts;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t d0 = (4 * g + i) * N;
+          if (d0 >= a.d) continue;
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            const float x = element<T, E4M3>(row, d0 + e);
+            if (fabsf(x) < __builtin_inff()) continue;
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+              if (key >= lo[t] && key < hi[t]) o[t][e][i] += x;
+          }
+        }
+      }
+    }
+  }
+  if (__ballot(skipped) && lane == 0) report(a.status, TUTTI_ST_BAD_BLOCK);
+
+  // the four wavefronts' maxima, sums and rows meet in LDS, 16 rows at a time
+  constexpr int LD = DP + 4;                        // rows apart by 4 banks
+  __shared__ __attribute__((aligned(16))) float rows[kAttendWaves][16][LD];
+  __shared__ float ml[kAttendWaves][16][2];
+  constexpr uint32_t EACH = 8, SEGS = DP / EACH;    // a thread joins 8 values of a row
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const float own_sum = sum_over_rows(l[t]);
+    if (t) __syncthreads();
+    if (g == 0) {
+      ml[wave][r][0] = m[t];
+      ml[wave][r][1] = own_sum;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int n = 0; n < N; n += 4)
+        *reinterpret_cast<f32x4 *>(&rows[wave][r][(4 * g + i) * N + n]) =
+            f32x4{o[t][n][i], o[t][n + 1][i], o[t][n + 2][i], o[t][n + 3][i]};
+    __syncthreads();
+    const uint32_t row_in = threadIdx.x / SEGS, e = (threadIdx.x % SEGS) * EACH, row = row_a + t * 16 + row_in;
+    if (row_in >= 16 || row >= n_rows || e >= a.d) continue;
+    float top = kLowest;
+#pragma unroll
+    for (uint32_t w = 0; w < kAttendWaves; ++w) top = fmaxf(top, ml[w][row_in][0]);
+    float sum = 0.0f, y[EACH] = {};
+#pragma unroll
+    for (uint32_t w = 0; w < kAttendWaves; ++w) {
+      const float by = __builtin_amdgcn_exp2f(ml[w][row_in][0] - top);
+      sum += by * ml[w][row_in][1];
+#pragma unroll
+      for (uint32_t i = 0; i < EACH; ++i) y[i] += by * rows[w][row_in][e + i];
+    }
+    if (u.parts > 1) {
+      const uint64_t at = static_cast<uint64_t>(u.part_slot + u.part) * ROWS + t * 16 + row_in;
+      float *to = a.part_o + at * DP + e;
+      *reinterpret_cast<f32x4 *>(to) = f32x4{y[0], y[1], y[2], y[3]};
+      *reinterpret_cast<f32x4 *>(to + 4) = f32x4{y[4], y[5], y[6], y[7]};
+      if (e == 0) a.part_ml[at] = f32x2{top, sum};
+      continue;
+    }
+    const uint32_t i = row / a.group, head = u.head * a.group + row - i * a.group;
+    const float by = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    typename T::eight z;
+#pragma unroll
+    for (uint32_t c = 0; c < EACH; ++c) z[c] = static_cast<typename T::one>(y[c] * by);
+    *reinterpret_cast<u32x4 *>(static_cast<uint8_t *>(a.out.base) + static_cast<uint64_t>(s.row0 + i) * a.out.row_stride +
+                               head * a.out.head_stride + 2 * e) = __builtin_bit_cast(u32x4, z);
+    if (e == 0 && a.lse)
+      a.lse[static_cast<uint64_t>(s.row0 + i) * (a.kv_heads * a.group) + head] =
+          sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+  }
+}
+
+// ---- Joins the parts of sequences that were split: one wavefront a row, DP/64 values a lane.
+template <typename T, int DP, int ROWS>
+__global__ __launch_bounds__(256) void k_kv_join(const AttendArgs a) {
+  const uint32_t lane = threadIdx.x & (kLanes - 1);
+  const uint32_t item = blockIdx.x * 4u + uniform(threadIdx.x / kLanes);
+  const Plan plan = make_plan<ROWS>(a);
+  // items: rows of the sequences that are split
+  uint32_t before = 0, slots = 0, units = 0;
+  for (uint32_t base = 0; base < a.batch.n_seq; base += kLanes) {
+    tutti_seq s{};
+    uint32_t n = 0, split = 0, parts = 0, all = 0;
+    if (base + lane < a.batch.n_seq) {
+      s = load_seq(a.batch.seqs + base + lane);
+      if (seq_ok(a.batch, s) && s.n_new) {
+        parts = parts_of(a, plan, s);
+        all = row_tiles<ROWS>(a, s) * a.kv_heads * parts;
+        if (parts > 1) {
+          n = s.n_new * a.group * a.kv_heads;
+          split = all;
+        }
+      }
+    }
+    const uint32_t upto = before + lane_prefix_sum(n), split_upto = slots + lane_prefix_sum(split);
+    const uint32_t units_upto = units + lane_prefix_sum(all);
+    const uint64_t behind = __ballot(n != 0 && upto > item);
+    if (behind) {
+      const uint32_t l = static_cast<uint32_t>(__builtin_ctzll(behind));
+      const uint32_t local = item - (from_lane(upto, l) - from_lane(n, l));
+      const uint32_t row0 = from_lane(s.row0, l), parts_l = from_lane(parts, l);
+      const uint32_t heads = a.group * a.kv_heads, i = local / heads, head = local - i * heads;
+      const uint32_t kv = head / a.group, row = i * a.group + head - kv * a.group;
+      const uint32_t slot = from_lane(split_upto, l) - from_lane(split, l) + (row / ROWS * a.kv_heads + kv) * parts_l;
+      // what the attention kernel did not do is not joined
+      if (slot + parts_l > a.max_parts || from_lane(units_upto, l) > a.max_units) return;
+      const uint64_t at0 = static_cast<uint64_t>(slot) * ROWS + row % ROWS;
+      float top = kLowest;
+      for (uint32_t p = lane; p < parts_l; p += kLanes) top = fmaxf(top, a.part_ml[at0 + static_cast<uint64_t>(p) * ROWS][0]);
+#pragma unroll
+      for (int x = 1; x < static_cast<int>(kLanes); x <<= 1) top = fmaxf(top, __shfl_xor(top, x, kLanes));
+      float sum = 0.0f;
+      constexpr int E = DP / 64;
+      float y[E] = {};
+#pragma unroll 4
+      for (uint32_t p = 0; p < parts_l; ++p) {
+        const uint64_t at = at0 + static_cast<uint64_t>(p) * ROWS;
+        const f32x2 ml = a.part_ml[at];
+        const float by = __builtin_amdgcn_exp2f(ml[0] - top);
+        sum += by * ml[1];
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (lane * E + e < a.d) y[e] += by * a.part_o[at * DP + lane * E + e];
+      }
+      const float by = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+      uint8_t *to = static_cast<uint8_t *>(a.out.base) + static_cast<uint64_t>(row0 + i) * a.out.row_stride + head * a.out.head_stride;
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (lane * E + e < a.d) reinterpret_cast<typename T::one *>(to)[lane * E + e] = static_cast<typename T::one>(y[e] * by);
+      if (lane == 0 && a.lse)
+        a.lse[static_cast<uint64_t>(row0 + i) * heads + head] =
+            sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+      return;
+    }
+    before = from_lane(upto, kLanes - 1);
+    slots = from_lane(split_upto, kLanes - 1);
+    units = from_lane(units_upto, kLanes - 1);
+  }
+}
+
+}  // namespace tutti

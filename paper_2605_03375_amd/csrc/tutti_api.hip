@@ -23,6 +23,7 @@
 #ifdef TUTTI_BENCH_BUILD
 #include "tutti_bench.h"
 #endif
+#include "library_state.h"
 #include "tutti_kernels.hip.h"
 
 // Bitmap of tutti_table_validate_static: one bit per pool block, kept by the library on every GPU it runs on.
@@ -2033,3 +2034,8 @@ int tutti_abi_describe(uint32_t *out, uint32_t cap) {
 }
 
 }  // extern "C"
+
+namespace tutti {
+int hip_failed(int hip_error) { return hip_fail(static_cast<hipError_t>(hip_error)); }
+int compute_units() { return cu_count(); }
+}  // namespace tutti
