@@ -594,8 +594,8 @@ typedef struct tutti_seq {
 
 /* A step's sequences (host record, device arrays).  max_new: no sequence has more new tokens than this.  n_rows: rows of q, k,
  * v and out; the sequences' n_new add up to at most that.  Skipped with TUTTI_ST_BAD_EXTENT, nothing of theirs written: a
- * sequence with n_new > max_new, n_new > n_held, row0 + n_new > n_rows or 2^31 tokens and more, and what is beyond n_rows where
- * the n_new add up to more (then which part of the sequences is skipped is not said). */
+ * sequence with n_new > max_new, n_new > n_held, row0 + n_new > n_rows or 2^31 tokens and more.  Where the n_new add up to more
+ * than n_rows, tokens of some of the sequences may be skipped in the same way. */
 typedef struct tutti_batch {
   const tutti_seq *d_seqs;
   const uint32_t *d_block_table;

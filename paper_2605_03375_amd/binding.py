@@ -822,7 +822,9 @@ def tutti_host_cost_of_restore(pool, cfg, d_n_blocks, n_req, d_block_table, tabl
 _FAST_NAMES = ["tutti_layer_restore", "tutti_layer_save", "tutti_obj_layout", "tutti_obj_pack", "tutti_obj_unpack",
                "tutti_sqe_build", "tutti_iocb_fill_direct", "tutti_issue_io", "tutti_issue_io_chained",
                "tutti_retrieve_layer", "tutti_store_layer", "tutti_retrieve_layer_issue", "tutti_store_layer_issue",
-               "tutti_retrieve_layer_chained", "tutti_store_layer_chained", "tutti_complete_io"]
+               "tutti_retrieve_layer_chained", "tutti_store_layer_chained", "tutti_complete_io", "tutti_kv_append",
+               "tutti_kv_attend"]
+_RECORDS = (tutti_pool, tutti_objcfg, tutti_ring, tutti_filestore, tutti_batch, tutti_rows, tutti_scales, tutti_rope, tutti_attn)
 _fast_call = None
 
 
@@ -835,7 +837,7 @@ def _wrap_fast(module, name, slow):
 def _form(argtypes):
     """Argument types of an entry point as the extension module writes them (fast_call.cpp, Entry::form)."""
     words = {C.c_void_p: "p", C.c_uint32: "i", C.c_uint64: "l"}
-    words.update({C.POINTER(t): str(i) for i, t in enumerate((tutti_pool, tutti_objcfg, tutti_ring, tutti_filestore))})
+    words.update({C.POINTER(t): str(i) for i, t in enumerate(_RECORDS)})
     return "".join(words.get(t, "?") for t in argtypes)
 
 
@@ -861,8 +863,7 @@ def _bind_fast_calls():
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     if raw is None:
         return
-    _fast_call.setup((tutti_pool, tutti_objcfg, tutti_ring, tutti_filestore), torch.Tensor, torch._C._cuda_getDevice, raw,
-                     _check)
+    _fast_call.setup(_RECORDS, torch.Tensor, torch._C._cuda_getDevice, raw, _check)
     for name in _FAST_NAMES:
         fn = getattr(_LIB, name)
         same = _fast_call.form(name) == _form(fn.argtypes)   # else the call stays with the ctypes wrapper

@@ -27,11 +27,12 @@
 
 namespace {
 
-enum Kind : uint8_t { kPointer, kStruct, kInt };
+enum Kind : uint8_t { kPointer, kStruct, kOptional, kInt };  // kOptional: a record, or what a pointer may be (None: no record)
 constexpr size_t kMaxArgs = 24;
+constexpr int kRecords = 9, kRequired = 4;  // classes of records; the first ones are always given as such
 
 // What the module has been told: classes of the C records, torch's functions, binding.py's error check.
-PyObject *g_records[4];  // tutti_pool, tutti_objcfg, tutti_ring, tutti_filestore
+PyObject *g_records[kRecords];  // in the order of record_of()
 PyObject *g_tensor_type, *g_get_device, *g_raw_stream, *g_check;
 std::atomic<bool> g_ready{false};  // the product library is the one in use, and torch has initialised the device here
 
@@ -40,7 +41,8 @@ template <typename A>
 constexpr int record_of() {
   using T = std::remove_cv_t<std::remove_pointer_t<A>>;
   return std::is_same_v<T, tutti_pool> ? 0 : std::is_same_v<T, tutti_objcfg> ? 1 : std::is_same_v<T, tutti_ring> ? 2
-         : std::is_same_v<T, tutti_filestore> ? 3 : -1;
+         : std::is_same_v<T, tutti_filestore> ? 3 : std::is_same_v<T, tutti_batch> ? 4 : std::is_same_v<T, tutti_rows> ? 5
+         : std::is_same_v<T, tutti_scales> ? 6 : std::is_same_v<T, tutti_rope> ? 7 : std::is_same_v<T, tutti_attn> ? 8 : -1;
 }
 
 // Arguments as 64-bit words; the last one is the stream.
@@ -49,7 +51,7 @@ struct Entry {
   size_t n;
   Kind kind[kMaxArgs];
   int8_t record[kMaxArgs];
-  char form[kMaxArgs + 1];  // what binding.py compares with the ctypes declaration: 0 to 3 a record, p a pointer, i / l 32 / 64 bits
+  char form[kMaxArgs + 1];  // what binding.py compares with the ctypes declaration: 0 to 8 a record, p a pointer, i / l 32 / 64 bits
   int (*invoke)(void *fn, const uint64_t *word);
 };
 
@@ -71,7 +73,8 @@ Entry entry(const char *name, int (*)(A...)) {
   static_assert(sizeof...(A) <= kMaxArgs);
   Entry e{name, sizeof...(A), {}, {}, {}, nullptr};
   size_t i = 0;
-  ((e.kind[i] = record_of<A>() >= 0 ? kStruct : std::is_pointer_v<A> ? kPointer : kInt, e.record[i] = record_of<A>(),
+  ((e.kind[i] = record_of<A>() >= kRequired ? kOptional : record_of<A>() >= 0 ? kStruct : std::is_pointer_v<A> ? kPointer : kInt,
+    e.record[i] = record_of<A>(),
     e.form[i] = record_of<A>() >= 0 ? static_cast<char>('0' + record_of<A>())
                 : std::is_pointer_v<A> ? 'p' : sizeof(A) == 4 ? 'i' : sizeof(A) == 8 ? 'l' : '?',
     ++i), ...);
@@ -87,7 +90,7 @@ const Entry kEntries[] = {
     ENTRY(tutti_iocb_fill_direct),       ENTRY(tutti_issue_io),             ENTRY(tutti_issue_io_chained),
     ENTRY(tutti_retrieve_layer),         ENTRY(tutti_store_layer),          ENTRY(tutti_retrieve_layer_issue),
     ENTRY(tutti_store_layer_issue),      ENTRY(tutti_retrieve_layer_chained), ENTRY(tutti_store_layer_chained),
-    ENTRY(tutti_complete_io),
+    ENTRY(tutti_complete_io),            ENTRY(tutti_kv_append),            ENTRY(tutti_kv_attend),
 };
 #undef ENTRY
 
@@ -133,7 +136,7 @@ bool stream_word(uint64_t *out) {  // torch's current stream
 }
 
 struct Views {
-  Py_buffer view[4];
+  Py_buffer view[kMaxArgs];
   int n = 0;
   ~Views() {
     while (n > 0) PyBuffer_Release(&view[--n]);
@@ -160,10 +163,10 @@ bool read_words(const Call *c, PyObject *const *args, size_t n_pos, PyObject *kw
     } else if (e.kind[i] == kInt) {
       if (!PyLong_CheckExact(x)) return false;
       word[i] = PyLong_AsUnsignedLongLongMask(x);
-    } else if (e.kind[i] == kPointer) {
+    } else if (e.kind[i] == kPointer || (e.kind[i] == kOptional && reinterpret_cast<PyObject *>(Py_TYPE(x)) != g_records[e.record[i]])) {
       if (!pointer_word(x, &word[i])) return false;
     } else {
-      if (reinterpret_cast<PyObject *>(Py_TYPE(x)) != g_records[e.record[i]] || views->n == 4) return false;
+      if (reinterpret_cast<PyObject *>(Py_TYPE(x)) != g_records[e.record[i]]) return false;
       if (PyObject_GetBuffer(x, &views->view[views->n], PyBUF_SIMPLE) != 0) {
         PyErr_Clear();
         return false;
@@ -269,11 +272,17 @@ PyObject *bind(PyObject *, PyObject *args) {
   Py_RETURN_NONE;
 }
 
-// setup(records, tensor type, function: current device, function: its current stream's handle, function: error check)
+// setup(records, tensor type, function: current device, function: its current stream's handle, function: error check).  Of the
+// records the first kRequired have to be named; a class that is not named is not recognised.
 PyObject *setup(PyObject *, PyObject *args) {
-  PyObject *r[4], *o[4];
-  if (!PyArg_ParseTuple(args, "(OOOO)OOOO", &r[0], &r[1], &r[2], &r[3], &o[0], &o[1], &o[2], &o[3])) return nullptr;
-  for (int i = 0; i < 4; ++i) Py_XSETREF(g_records[i], Py_NewRef(r[i]));
+  PyObject *r, *o[4];
+  if (!PyArg_ParseTuple(args, "O!OOOO", &PyTuple_Type, &r, &o[0], &o[1], &o[2], &o[3])) return nullptr;
+  if (PyTuple_GET_SIZE(r) < kRequired || PyTuple_GET_SIZE(r) > kRecords) {
+    PyErr_SetString(PyExc_ValueError, "setup: another number of record classes");
+    return nullptr;
+  }
+  for (int i = 0; i < kRecords; ++i)
+    Py_XSETREF(g_records[i], i < PyTuple_GET_SIZE(r) ? Py_NewRef(PyTuple_GET_ITEM(r, i)) : nullptr);
   PyObject **const to[4] = {&g_tensor_type, &g_get_device, &g_raw_stream, &g_check};
   for (int i = 0; i < 4; ++i) Py_XSETREF(*to[i], Py_NewRef(o[i]));
   Py_RETURN_NONE;

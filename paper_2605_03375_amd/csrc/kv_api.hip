@@ -82,12 +82,32 @@ int launched() {
 
 // ---- append
 
-template <typename T, bool E4M3>
-void launch_append(const AppendArgs &a, uint32_t grid, hipStream_t stream) {
-  if (a.d <= 64)
-    hipLaunchKernelGGL((k_kv_append<T, E4M3, 8>), dim3(grid), dim3(256), 0, stream, a);
+template <typename T, bool E4M3, int LPR>
+void launch_append(const AppendArgs &a, int turn, uint32_t grid, hipStream_t stream) {
+  const dim3 g(grid), wg(256);
+  if (turn == kNoTurn)
+    hipLaunchKernelGGL((k_kv_append<T, E4M3, LPR, kNoTurn>), g, wg, 0, stream, a);
+  else if (turn == kHalves)
+    hipLaunchKernelGGL((k_kv_append<T, E4M3, LPR, kHalves>), g, wg, 0, stream, a);
+  else if (turn == kPairs)
+    hipLaunchKernelGGL((k_kv_append<T, E4M3, LPR, kPairs>), g, wg, 0, stream, a);
   else
-    hipLaunchKernelGGL((k_kv_append<T, E4M3, 16>), dim3(grid), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((k_kv_append<T, E4M3, LPR, kAnyTurn>), g, wg, 0, stream, a);
+}
+template <typename T>
+void launch_append(const AppendArgs &a, bool e4m3, int turn, uint32_t grid, hipStream_t stream) {
+  if (e4m3)
+    a.d <= 64 ? launch_append<T, true, 8>(a, turn, grid, stream) : launch_append<T, true, 16>(a, turn, grid, stream);
+  else
+    a.d <= 64 ? launch_append<T, false, 8>(a, turn, grid, stream) : launch_append<T, false, 16>(a, turn, grid, stream);
+}
+
+// How the rotation's pairs lie for lanes that take 8 values each.
+int turn_of(const RopeView &r) {
+  if (r.rot == 0) return kNoTurn;
+  const uint32_t all = r.half | r.end[0] | r.end[1] | r.end[2];
+  if (!r.interleaved) return all % 8 == 0 ? kHalves : kAnyTurn;
+  return all % 4 == 0 ? kPairs : kAnyTurn;
 }
 
 // ---- attend
@@ -198,20 +218,21 @@ int tutti_kv_append(const tutti_pool *pool, const tutti_scales *scales, const tu
   a.d = pool->head_dim;
   a.status = d_status;
   const bool e4m3 = scales != nullptr;
+  // a unit has at least one new token, and only a sequence's first and last may have fewer than a whole unit's
+  const uint64_t tokens = e4m3 ? pool->block_tokens : kLanes / (a.d <= 64 ? 8 : 16);
+  uint64_t units = std::min<uint64_t>(batch->n_rows, batch->n_rows / tokens + 2ull * batch->n_seq);
+  if (batch->max_new == 1) units = batch->n_seq;
   a.heads_a_job = 4;
   a.q_jobs = (a.q_heads + a.heads_a_job - 1) / a.heads_a_job;
   a.jobs = a.q_jobs + 2 * (e4m3 ? a.kv_heads : (a.kv_heads + a.heads_a_job - 1) / a.heads_a_job);
-  // a unit has at least one new token, and only a sequence's first and last may have fewer than a whole unit's
-  const uint64_t tokens = e4m3 ? pool->block_tokens : kLanes / (a.d <= 64 ? 8 : 16);
-  const uint64_t units = std::min<uint64_t>(batch->n_rows, batch->n_rows / tokens + 2ull * batch->n_seq);
   if (units * a.jobs >= 0x80000000ull) return TUTTI_ERANGE;
   a.max_units = static_cast<uint32_t>(units);
   const uint32_t grid = static_cast<uint32_t>((units * a.jobs + 3) / 4);
   const hipStream_t st = static_cast<hipStream_t>(stream);
   if (dtype == TUTTI_BF16)
-    e4m3 ? launch_append<Bf16, true>(a, grid, st) : launch_append<Bf16, false>(a, grid, st);
+    launch_append<Bf16>(a, e4m3, turn_of(a.rope), grid, st);
   else
-    e4m3 ? launch_append<Fp16, true>(a, grid, st) : launch_append<Fp16, false>(a, grid, st);
+    launch_append<Fp16>(a, e4m3, turn_of(a.rope), grid, st);
   return launched();
 }
 

@@ -72,6 +72,12 @@ __device__ __forceinline__ bool seq_ok(const BatchView &b, const tutti_seq &s) {
          s.n_held < 0x80000000u;
 }
 
+// The record at a wavefront's own address, by the scalar path.
+__device__ __forceinline__ tutti_seq uniform_seq(const tutti_seq *s) {
+  const u32x4 w = *constant(reinterpret_cast<const u32x4 *>(s));
+  return tutti_seq{w[0], w[1], w[2], w[3]};
+}
+
 // Inclusive sum over the wavefront's lanes: data-parallel moves inside rows of 16 lanes, then across them.
 template <int CTRL, int ROWS>
 __device__ __forceinline__ uint32_t moved_or_0(uint32_t v) {
