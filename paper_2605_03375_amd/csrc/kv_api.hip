@@ -148,8 +148,14 @@ int check_attn(const tutti_pool *pool, const tutti_attn *attn) {
 template <typename T, bool E4M3, int DP, bool PAGED16, int RT>
 void launch_attend(const AttendArgs &a, hipStream_t stream) {
   hipLaunchKernelGGL((k_kv_attend<T, E4M3, DP, PAGED16, RT>), dim3(a.max_units), dim3(256), 0, stream, a);
-  const uint32_t joins = (a.batch.n_rows * a.kv_heads * a.group + 3) / 4;
-  hipLaunchKernelGGL((k_kv_join<T, DP, RT * 16>), dim3(joins), dim3(256), 0, stream, a);
+  // a sequence that is split has two parts or more to a row tile, so no more rows are to be joined than this
+  const uint32_t joins = std::min(a.batch.n_rows * a.kv_heads * a.group, a.max_parts / 2 * RT * 16);
+  // a workgroup a row for few rows, which may have many parts (32 rows of 128 parts: 6.7 us; one wavefront, part after part, 75);
+  // else a wavefront a row (1,511 queries of 20 heads in two parts: 20 us, with workgroups 61)
+  if (joins <= 4096)
+    hipLaunchKernelGGL((k_kv_join<T, DP, RT * 16, 4>), dim3(joins), dim3(256), 0, stream, a);
+  else
+    hipLaunchKernelGGL((k_kv_join<T, DP, RT * 16, 1>), dim3((joins + 3) / 4), dim3(256), 0, stream, a);
 }
 template <typename T, bool E4M3, int DP>
 void launch_attend(const AttendArgs &a, uint32_t rows, hipStream_t stream) {

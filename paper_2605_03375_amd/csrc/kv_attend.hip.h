@@ -554,23 +554,28 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(const AttendArgs a) {
   }
 }
 
-// ---- Joins the parts of sequences that were split: one wavefront a row, DP/64 values a lane.
-template <typename T, int DP, int ROWS>
+// ---- Joins the parts of sequences that were split: one workgroup (WAVES 4) or one wavefront (1) a row.  DP/4 threads take a
+// part, four values each; so many parts go abreast, and four times that many are under way at once.
+template <typename T, int DP, int ROWS, int WAVES>
 __global__ __launch_bounds__(256) void k_kv_join(const AttendArgs a) {
-  const uint32_t lane = threadIdx.x & (kLanes - 1);
-  const uint32_t item = blockIdx.x * 4u + uniform(threadIdx.x / kLanes);
+  constexpr uint32_t TP = DP / 4, ABREAST = WAVES * kLanes / TP, U = 4;
+  const uint32_t lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
+  const uint32_t item = WAVES == 4 ? blockIdx.x : blockIdx.x * 4 + uniform(wave);
+  const uint32_t thread = WAVES == 4 ? threadIdx.x : lane;   // among those of the row
   const Plan plan = make_plan<ROWS>(a);
   // items: rows of the sequences that are split
   uint32_t before = 0, slots = 0, units = 0;
-  for (uint32_t base = 0; base < a.batch.n_seq; base += kLanes) {
+  bool found = false;
+  uint32_t row0 = 0, parts = 0, local = 0, first_slot = 0, units_upto_it = 0;
+  for (uint32_t base = 0; base < a.batch.n_seq && !found; base += kLanes) {
     tutti_seq s{};
-    uint32_t n = 0, split = 0, parts = 0, all = 0;
+    uint32_t n = 0, split = 0, p = 0, all = 0;
     if (base + lane < a.batch.n_seq) {
       s = load_seq(a.batch.seqs + base + lane);
       if (seq_ok(a.batch, s) && s.n_new) {
-        parts = parts_of(a, plan, s);
-        all = row_tiles<ROWS>(a, s) * a.kv_heads * parts;
-        if (parts > 1) {
+        p = parts_of(a, plan, s);
+        all = row_tiles<ROWS>(a, s) * a.kv_heads * p;
+        if (p > 1) {
           n = s.n_new * a.group * a.kv_heads;
           split = all;
         }
@@ -581,45 +586,85 @@ __global__ __launch_bounds__(256) void k_kv_join(const AttendArgs a) {
     const uint64_t behind = __ballot(n != 0 && upto > item);
     if (behind) {
       const uint32_t l = static_cast<uint32_t>(__builtin_ctzll(behind));
-      const uint32_t local = item - (from_lane(upto, l) - from_lane(n, l));
-      const uint32_t row0 = from_lane(s.row0, l), parts_l = from_lane(parts, l);
-      const uint32_t heads = a.group * a.kv_heads, i = local / heads, head = local - i * heads;
-      const uint32_t kv = head / a.group, row = i * a.group + head - kv * a.group;
-      const uint32_t slot = from_lane(split_upto, l) - from_lane(split, l) + (row / ROWS * a.kv_heads + kv) * parts_l;
-      // what the attention kernel did not do is not joined
-      if (slot + parts_l > a.max_parts || from_lane(units_upto, l) > a.max_units) return;
-      const uint64_t at0 = static_cast<uint64_t>(slot) * ROWS + row % ROWS;
-      float top = kLowest;
-      for (uint32_t p = lane; p < parts_l; p += kLanes) top = fmaxf(top, a.part_ml[at0 + static_cast<uint64_t>(p) * ROWS][0]);
-#pragma unroll
-      for (int x = 1; x < static_cast<int>(kLanes); x <<= 1) top = fmaxf(top, __shfl_xor(top, x, kLanes));
-      float sum = 0.0f;
-      constexpr int E = DP / 64;
-      float y[E] = {};
-#pragma unroll 4
-      for (uint32_t p = 0; p < parts_l; ++p) {
-        const uint64_t at = at0 + static_cast<uint64_t>(p) * ROWS;
-        const f32x2 ml = a.part_ml[at];
-        const float by = __builtin_amdgcn_exp2f(ml[0] - top);
-        sum += by * ml[1];
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (lane * E + e < a.d) y[e] += by * a.part_o[at * DP + lane * E + e];
-      }
-      const float by = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-      uint8_t *to = static_cast<uint8_t *>(a.out.base) + static_cast<uint64_t>(row0 + i) * a.out.row_stride + head * a.out.head_stride;
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (lane * E + e < a.d) reinterpret_cast<typename T::one *>(to)[lane * E + e] = static_cast<typename T::one>(y[e] * by);
-      if (lane == 0 && a.lse)
-        a.lse[static_cast<uint64_t>(row0 + i) * heads + head] =
-            sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * kLn2;
-      return;
+      found = true;
+      local = item - (from_lane(upto, l) - from_lane(n, l));
+      row0 = from_lane(s.row0, l);
+      parts = from_lane(p, l);
+      first_slot = from_lane(split_upto, l) - from_lane(split, l);
+      units_upto_it = from_lane(units_upto, l);
     }
     before = from_lane(upto, kLanes - 1);
     slots = from_lane(split_upto, kLanes - 1);
     units = from_lane(units_upto, kLanes - 1);
   }
+  if (!found) return;
+  const uint32_t heads = a.group * a.kv_heads, i = local / heads, head = local - i * heads;
+  const uint32_t kv = head / a.group, row = i * a.group + head - kv * a.group;
+  const uint32_t slot = first_slot + (row / ROWS * a.kv_heads + kv) * parts;
+  // what the attention kernel did not do is not joined
+  if (slot + parts > a.max_parts || units_upto_it > a.max_units) return;
+  const uint64_t at0 = static_cast<uint64_t>(slot) * ROWS + row % ROWS;
+
+  float top = kLowest;
+  for (uint32_t p = thread; p < parts; p += WAVES * kLanes) top = fmaxf(top, a.part_ml[at0 + static_cast<uint64_t>(p) * ROWS][0]);
+#pragma unroll
+  for (int x = 1; x < 16; x <<= 1) top = fmaxf(top, __shfl_xor(top, x, kLanes));
+  top = max_over_rows(top);
+  __shared__ float tops[4], sums[4 * kLanes / TP];
+  __shared__ __attribute__((aligned(16))) float half[4 * kLanes / TP][DP];
+  if constexpr (WAVES == 4) {
+    if (lane == 0) tops[wave] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+  }
+  const uint32_t e = thread % TP * 4, mine = thread / TP;
+  float sum = 0.0f;
+  f32x4 y = {0, 0, 0, 0};
+  if (e < a.d) {
+    for (uint32_t p0 = mine; p0 < parts; p0 += U * ABREAST) {
+      f32x2 ml[U];
+      f32x4 o[U];
+#pragma unroll
+      for (uint32_t u = 0; u < U; ++u)
+        if (p0 + u * ABREAST < parts) {
+          const uint64_t at = at0 + static_cast<uint64_t>(p0 + u * ABREAST) * ROWS;
+          ml[u] = a.part_ml[at];
+          o[u] = *reinterpret_cast<const f32x4 *>(a.part_o + at * DP + e);
+        }
+#pragma unroll
+      for (uint32_t u = 0; u < U; ++u)
+        if (p0 + u * ABREAST < parts) {
+          const float by = __builtin_amdgcn_exp2f(ml[u][0] - top);
+          sum += by * ml[u][1];
+          y += by * o[u];
+        }
+    }
+  }
+  // the parts that went abreast: in LDS, a wavefront in its own rows of it
+  const uint32_t first = WAVES == 4 ? 0 : uniform(wave) * ABREAST;
+  *reinterpret_cast<f32x4 *>(&half[first + mine][e]) = y;
+  if (e == 0) sums[first + mine] = sum;
+  if constexpr (WAVES == 4) {
+    __syncthreads();
+  } else {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+  if (thread * 2 >= a.d) return;
+  float total = 0.0f;
+  f32x2 z = {0, 0};
+#pragma unroll
+  for (uint32_t w = 0; w < ABREAST; ++w) {
+    total += sums[first + w];
+    z += *reinterpret_cast<const f32x2 *>(&half[first + w][2 * thread]);
+  }
+  const float by = total > 0.0f || total != total ? 1.0f / total : 0.0f;
+  uint8_t *to = static_cast<uint8_t *>(a.out.base) + static_cast<uint64_t>(row0 + i) * a.out.row_stride + head * a.out.head_stride;
+  reinterpret_cast<typename T::two *>(to)[thread] =
+      typename T::two{static_cast<typename T::one>(z[0] * by), static_cast<typename T::one>(z[1] * by)};
+  if (thread == 0 && a.lse)
+    a.lse[static_cast<uint64_t>(row0 + i) * heads + head] =
+        total == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
 }  // namespace tutti
