@@ -117,8 +117,16 @@ uint32_t rows_a_tile(const tutti_batch *b, uint32_t group) {
   return static_cast<uint64_t>(b->max_new) * group <= 16 ? 16 : 32;
 }
 
+// Neighbouring KV heads that a workgroup takes side by side, so that it reads stretches of a block and not a head's rows here and
+// there (128-byte rows of 8 heads: 4.7 TB/s one head a workgroup, 5.8 with four side by side, 6.0 with eight).
+uint32_t heads_abreast(uint32_t kv_heads) {
+  for (uint32_t n : {4u, 5u, 3u, 2u})
+    if (kv_heads % n == 0) return n;
+  return 1;
+}
+
 struct AttendSizes {
-  uint32_t rows, dp, target, max_units, max_parts;
+  uint32_t rows, dp, abreast, key_waves, target, max_units, max_parts;
   uint64_t ml_bytes, bytes;
 };
 
@@ -128,12 +136,14 @@ int attend_sizes(const tutti_pool *pool, const tutti_batch *b, const tutti_attn 
   const uint32_t group = attn->n_q_heads / pool->num_kv_heads;
   s->rows = rows_a_tile(b, group);
   s->dp = pool->head_dim <= 64 ? 64 : 128;
-  s->target = 1024;
+  s->abreast = heads_abreast(pool->num_kv_heads);
+  s->key_waves = s->abreast == 1 ? 4 : s->abreast == 2 ? 2 : 1;
+  s->target = 768;  // three workgroups a compute unit: what fits of most kernels
   const uint64_t tiles = static_cast<uint64_t>(b->n_rows) * group / s->rows + std::min(b->n_seq, b->n_rows);
-  const uint64_t units = s->target + tiles * pool->num_kv_heads;
+  const uint64_t units = s->target + tiles * (pool->num_kv_heads / s->abreast);
   if (units >= 0x80000000ull || static_cast<uint64_t>(b->n_rows) * attn->n_q_heads >= 0x80000000ull) return TUTTI_ERANGE;
   s->max_units = static_cast<uint32_t>(units);
-  s->max_parts = 2 * s->target;
+  s->max_parts = 2 * s->target * s->abreast;
   s->ml_bytes = static_cast<uint64_t>(s->max_parts) * s->rows * sizeof(f32x2);
   s->bytes = s->ml_bytes + static_cast<uint64_t>(s->max_parts) * s->rows * s->dp * sizeof(float);
   return TUTTI_OK;
@@ -147,15 +157,22 @@ int check_attn(const tutti_pool *pool, const tutti_attn *attn) {
 
 template <typename T, bool E4M3, int DP, bool PAGED16, int RT>
 void launch_attend(const AttendArgs &a, hipStream_t stream) {
-  hipLaunchKernelGGL((k_kv_attend<T, E4M3, DP, PAGED16, RT>), dim3(a.max_units), dim3(256), 0, stream, a);
+  const dim3 grid(a.max_units), wg(64 * a.abreast * a.key_waves);
+  if (a.d == DP)
+    hipLaunchKernelGGL((k_kv_attend<T, E4M3, DP, true, PAGED16, RT>), grid, wg, 0, stream, a);
+  else
+    hipLaunchKernelGGL((k_kv_attend<T, E4M3, DP, false, PAGED16, RT>), grid, wg, 0, stream, a);
+}
+template <typename T, int DP, int ROWS>
+void launch_join(const AttendArgs &a, hipStream_t stream) {
   // a sequence that is split has two parts or more to a row tile, so no more rows are to be joined than this
-  const uint32_t joins = std::min(a.batch.n_rows * a.kv_heads * a.group, a.max_parts / 2 * RT * 16);
+  const uint32_t joins = std::min(a.batch.n_rows * a.kv_heads * a.group, a.max_parts / 2 * ROWS);
   // a workgroup a row for few rows, which may have many parts (32 rows of 128 parts: 6.7 us; one wavefront, part after part, 75);
   // else a wavefront a row (1,511 queries of 20 heads in two parts: 20 us, with workgroups 61)
   if (joins <= 4096)
-    hipLaunchKernelGGL((k_kv_join<T, DP, RT * 16, 4>), dim3(joins), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((k_kv_join<T, DP, ROWS, 4>), dim3(joins), dim3(256), 0, stream, a);
   else
-    hipLaunchKernelGGL((k_kv_join<T, DP, RT * 16, 1>), dim3((joins + 3) / 4), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((k_kv_join<T, DP, ROWS, 1>), dim3((joins + 3) / 4), dim3(256), 0, stream, a);
 }
 template <typename T, bool E4M3, int DP>
 void launch_attend(const AttendArgs &a, uint32_t rows, hipStream_t stream) {
@@ -163,6 +180,7 @@ void launch_attend(const AttendArgs &a, uint32_t rows, hipStream_t stream) {
     rows == 16 ? launch_attend<T, E4M3, DP, true, 1>(a, stream) : launch_attend<T, E4M3, DP, true, 2>(a, stream);
   else
     rows == 16 ? launch_attend<T, E4M3, DP, false, 1>(a, stream) : launch_attend<T, E4M3, DP, false, 2>(a, stream);
+  rows == 16 ? launch_join<T, DP, 16>(a, stream) : launch_join<T, DP, 32>(a, stream);
 }
 template <typename T>
 void launch_attend(const AttendArgs &a, bool e4m3, uint32_t rows, hipStream_t stream) {
@@ -275,6 +293,8 @@ int tutti_kv_attend(const tutti_pool *pool, const tutti_scales *scales, const tu
   a.scale_log2 = attn->sm_scale * kLog2e;
   a.causal = attn->causal;
   a.window = attn->window;
+  a.abreast = s.abreast;
+  a.key_waves = s.key_waves;
   a.target = s.target;
   a.min_tiles = 8;
   a.max_units = s.max_units;

@@ -7,7 +7,7 @@
 namespace tutti {
 
 constexpr uint32_t kKeyTile = 32;    // keys that a wavefront takes at a time: two halves of 16
-constexpr uint32_t kAttendWaves = 4; // wavefronts of a workgroup: every fourth tile each
+constexpr uint32_t kMostWaves = 5;   // wavefronts of a workgroup at most
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 // A row's running maximum is raised only by steps of more than this (log2): until then its weights are at most 2^8, far from
 // the largest fp16 value, and nothing that has been summed has to be rescaled.
@@ -19,6 +19,8 @@ struct AttendArgs {
   tutti_rows q, out;
   float *lse;
   uint32_t kv_heads, group, d;  // group: query heads of one KV head
+  // A workgroup: `abreast` neighbouring KV heads (a divisor of kv_heads), `key_waves` wavefronts each that take its tiles in turn.
+  uint32_t abreast, key_waves;
   float scale_log2;             // sm_scale * log2(e)
   uint32_t causal, window;
   // How the keys are split: a sequence's tiles go in parts of about max(min_tiles, all tiles / target) tiles.
@@ -59,7 +61,7 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs &a) {
   }
 #pragma unroll
   for (int m = 1; m < static_cast<int>(kLanes); m <<= 1) work += __shfl_xor(work, m, kLanes);
-  work *= a.kv_heads;
+  work *= a.kv_heads / a.abreast;
   const uint64_t each = (work + a.target - 1) / a.target;
   Plan p;
   p.tiles_a_part = uniform(each > 0x40000000u ? 0x40000000u : static_cast<uint32_t>(each));
@@ -76,8 +78,8 @@ __device__ __forceinline__ uint32_t parts_of(const AttendArgs &a, const Plan &p,
 struct Unit {
   uint32_t seq;         // n_seq: none
   tutti_seq s;
-  uint32_t row_tile, head, part, parts;
-  uint32_t part_slot;   // of its first part in the work memory, where parts > 1
+  uint32_t row_tile, head, part, parts;  // head: the first of its heads
+  uint32_t part_slot;   // of its first head's first part in the work memory, where parts > 1; the next head's are behind those
 };
 
 template <int ROWS>
@@ -97,8 +99,8 @@ __device__ __forceinline__ Unit locate(const AttendArgs &a, const Plan &p, uint3
       if (ok && s.n_new) {
         tiles = row_tiles<ROWS>(a, s);
         parts = parts_of(a, p, s);
-        n = tiles * a.kv_heads * parts;
-        split = parts > 1 ? n : 0;
+        n = tiles * (a.kv_heads / a.abreast) * parts;
+        split = parts > 1 ? tiles * a.kv_heads * parts : 0;
       }
     }
     const uint32_t upto = before + lane_prefix_sum(n), split_upto = slots + lane_prefix_sum(split);
@@ -110,9 +112,10 @@ __device__ __forceinline__ Unit locate(const AttendArgs &a, const Plan &p, uint3
       u.s = tutti_seq{from_lane(s.row0, l), from_lane(s.n_new, l), from_lane(s.n_held, l), from_lane(s.table_off, l)};
       u.parts = from_lane(parts, l);
       // heads first, then parts, then row tiles: neighbours read the same blocks
-      u.head = local % a.kv_heads;
-      u.part = local / a.kv_heads % u.parts;
-      u.row_tile = local / a.kv_heads / u.parts;
+      const uint32_t head_groups = a.kv_heads / a.abreast;
+      u.head = local % head_groups * a.abreast;
+      u.part = local / head_groups % u.parts;
+      u.row_tile = local / head_groups / u.parts;
       u.part_slot = from_lane(split_upto, l) - from_lane(split, l) + (u.row_tile * a.kv_heads + u.head) * u.parts;
       if (!first) return u;
     }
@@ -212,8 +215,8 @@ __device__ __forceinline__ void set_word(typename Words<N>::type &w, int i, uint
 // made them.  The contraction's order is free: a lane loads 16 consecutive bytes of a key's row, and the queries are laid out to
 // match.  Of the values, a lane takes DP/16 consecutive ones of its eight keys, and puts pairs of keys together by byte
 // permutations; so nothing passes through LDS and no wavefront waits for another until the end, where the four join.
-template <typename T, bool E4M3, int DP, bool PAGED16, int RT>
-__global__ __launch_bounds__(256, 2) void k_kv_attend(const AttendArgs a) {
+template <typename T, bool E4M3, int DP, bool FULL, bool PAGED16, int RT>
+__global__ __launch_bounds__(64 * kMostWaves, RT == 1 ? 3 : 2) void k_kv_attend(const AttendArgs a) {
   constexpr int ROWS = RT * 16, N = DP / 16;
   constexpr int KW = E4M3 ? DP / 64 : DP / 32;       // 16-byte loads of a key a lane does
   constexpr int VW = E4M3 ? N / 4 : N / 2;           // words of a value row a lane takes
@@ -228,12 +231,13 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(const AttendArgs a) {
   const Plan plan = make_plan<ROWS>(a);
   const Unit u = locate<ROWS>(a, plan, blockIdx.x, reporter);
   if (u.seq == a.batch.n_seq) return;
-  if (u.parts > 1 && u.part_slot + u.parts > a.max_parts) {
+  if (u.parts > 1 && u.part_slot + a.abreast * u.parts > a.max_parts) {
     if (threadIdx.x == 0) report(a.status, TUTTI_ST_BAD_EXTENT);
     return;
   }
   const tutti_seq s = u.s;
   const uint32_t begin = s.n_held - s.n_new, n_rows = s.n_new * a.group;
+  const uint32_t kv_head = u.head + wave % a.abreast, turn = wave / a.abreast;
 
   // the keys that this lane's rows see: [lo, hi)
   uint32_t lo[RT], hi[RT];
@@ -241,7 +245,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(const AttendArgs a) {
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     const uint32_t row = u.row_tile * ROWS + t * 16 + r;
-    const uint32_t i = row < n_rows ? row / a.group : 0, head = u.head * a.group + (row < n_rows ? row - i * a.group : 0);
+    const uint32_t i = row < n_rows ? row / a.group : 0, head = kv_head * a.group + (row < n_rows ? row - i * a.group : 0);
     const uint32_t place = begin + i;
     hi[t] = a.causal ? place + 1 : s.n_held;
     lo[t] = a.window && place + 1 > a.window ? place + 1 - a.window : 0;
@@ -266,7 +270,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(const AttendArgs a) {
     for (int j = 0; j < DP / 32; ++j) {
       const uint32_t e = E4M3 ? (j / 2) * 64 + g * 16 + (j & 1) * 8 : j * 32 + g * 8;
       u32x4 w = {0, 0, 0, 0};
-      if (e < a.d) w = *reinterpret_cast<const u32x4 *>(q_at[t] + 2 * e);
+      if (FULL || e < a.d) w = *reinterpret_cast<const u32x4 *>(q_at[t] + 2 * e);
       q[t][j] = __builtin_bit_cast(typename T::eight, w);
     }
 
@@ -280,146 +284,52 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(const AttendArgs a) {
     for (int n = 0; n < N; ++n) o[t][n] = f32x4{0, 0, 0, 0};
   }
 
-  const uint64_t head_at = static_cast<uint64_t>(u.head) * a.pool.head_stride;
+  const uint64_t head_at = static_cast<uint64_t>(kv_head) * a.pool.head_stride;
   const uint32_t ts = a.pool.token_stride;
+  // of a value's row a lane takes VW words; lanes beyond the row take its first ones (nothing is made of what they add)
+  const uint32_t v_in_row = FULL || r * (VW * 4) < a.d * EB ? r * (VW * 4) : 0;
   bool skipped = false;
-  for (uint32_t tile = t0 + wave; tile < t1; tile += kAttendWaves) {
-    const uint32_t key0 = tile * kKeyTile;
-    // the blocks: of each half tile (PAGED16: a half lies in one block), or of each key
-    float ck[2][4], cv[2][4], iv[2][4];              // factor of the scores, log2 and reciprocal of the values' scale
-    bool there[2][4];
-    const uint8_t *k_at[2], *v_at[2][4];
-    bool edge = key0 < all_lo || key0 + kKeyTile > all_hi;
-    if constexpr (PAGED16) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint32_t key = key0 + 16 * h;
-        const uint32_t n = block_of(a.pool, key);
-        const uint64_t at = static_cast<uint64_t>(s.table_off) + n;
-        uint32_t id = 0;
-        bool ok = key + 16 > any_lo && key < any_hi;
-        if (ok) {
-          ok = at < a.batch.table_len;
-          if (ok) {
-            id = constant(a.batch.table)[at];
-            ok = id < a.pool.num_blocks;
-            id = ok ? id : 0;
-          }
-          if (!ok) skipped = true;
-        }
-        if (!ok) edge = true;
-        const uint64_t off = id * a.pool.block_stride + head_at + static_cast<uint64_t>(key - n * a.pool.block_tokens) * ts;
-        k_at[h] = a.pool.k + off + r * ts;
-        float f = a.scale_log2, lg = 0.0f, rc = 1.0f;
-        if constexpr (E4M3) {
-          f *= constant(a.pool.k_scale)[id * a.pool.scale_stride + u.head];
-          const float sv = constant(a.pool.v_scale)[id * a.pool.scale_stride + u.head];
-          lg = __builtin_amdgcn_logf(sv);
-          rc = ok ? 1.0f / sv : 0.0f;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          v_at[h][i] = a.pool.v + off + (4 * g + i) * ts;
-          ck[h][i] = f;
-          cv[h][i] = lg;
-          iv[h][i] = rc;
-          there[h][i] = ok;
-        }
-      }
-    } else {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        // lane r looks up key r of the half; the others' come from it
-        const uint32_t key = key0 + 16 * h + r;
-        const uint32_t n = block_of(a.pool, key);
-        const uint64_t at = static_cast<uint64_t>(s.table_off) + n;
-        uint32_t id = 0;
-        bool ok = key >= any_lo && key < any_hi;
-        if (ok) {
-          ok = at < a.batch.table_len;
-          if (ok) {
-            id = a.batch.table[at];
-            ok = id < a.pool.num_blocks;
-            id = ok ? id : 0;
-          }
-          if (!ok) skipped = true;
-        }
-        if (__ballot(!ok)) edge = true;
-        const uint32_t slot = ok ? key - n * a.pool.block_tokens : 0;
-        k_at[h] = a.pool.k + id * a.pool.block_stride + head_at + static_cast<uint64_t>(slot) * ts;
-        float f = a.scale_log2, lg = 0.0f, rc = 1.0f;
-        if constexpr (E4M3) {
-          f *= a.pool.k_scale[id * a.pool.scale_stride + u.head];
-          const float sv = a.pool.v_scale[id * a.pool.scale_stride + u.head];
-          lg = __builtin_amdgcn_logf(sv);
-          rc = ok ? 1.0f / sv : 0.0f;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int from = static_cast<int>(4 * g + i);
-          const uint32_t id_i = __shfl(id, from, 16), slot_i = __shfl(slot, from, 16);
-          v_at[h][i] = a.pool.v + id_i * a.pool.block_stride + head_at + static_cast<uint64_t>(slot_i) * ts;
-          ck[h][i] = __shfl(f, from, 16);
-          cv[h][i] = __shfl(lg, from, 16);
-          iv[h][i] = __shfl(rc, from, 16);
-          there[h][i] = __shfl(static_cast<int>(ok), from, 16);
-        }
-      }
-    }
-    u32x4 kw[2][KW];
-    VWords vw[8];
+
+  // S^T of a tile
+  const auto scores = [&](const u32x4 (&kw)[2][KW], f32x4 (&sc)[RT][2]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
 #pragma unroll
+      for (int t = 0; t < RT; ++t) sc[t][h] = f32x4{0, 0, 0, 0};
+#pragma unroll
       for (int j = 0; j < KW; ++j) {
-        kw[h][j] = u32x4{0, 0, 0, 0};
-        if (j * 64 + g * 16 < a.d * EB) kw[h][j] = *reinterpret_cast<const u32x4 *>(k_at[h] + j * 64 + g * 16);
-      }
+        if constexpr (E4M3) {
+          const typename T::eight k0 = widen<T>(u32x2{kw[h][j][0], kw[h][j][1]}), k1 = widen<T>(u32x2{kw[h][j][2], kw[h][j][3]});
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        vw[4 * h + i] = VWords{};
-        if (r * (VW * 4) < a.d * EB) vw[4 * h + i] = *reinterpret_cast<const VWords *>(v_at[h][i] + r * (VW * 4));
-      }
-    }
-    // values of keys that no row sees are whatever lies there: nothing of them may reach a product, not even times 0
-    if (edge) {
+          for (int t = 0; t < RT; ++t) {
+            sc[t][h] = product<T>(k0, q[t][2 * j], sc[t][h]);
+            sc[t][h] = product<T>(k1, q[t][2 * j + 1], sc[t][h]);
+          }
+        } else {
+          const typename T::eight k0 = __builtin_bit_cast(typename T::eight, kw[h][j]);
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t key = key0 + 16 * h + 4 * g + i;
-          if (!there[h][i] || key < any_lo || key >= any_hi) vw[4 * h + i] = VWords{};
+          for (int t = 0; t < RT; ++t) sc[t][h] = product<T>(k0, q[t][j], sc[t][h]);
         }
+      }
     }
-    typename P::eight p[RT];
+  };
+  // weights of a tile, from its scores: c(h, i) holds the factor of key i of a lane's four in half h, the log2 and the reciprocal
+  // of its value's scale, and whether it is there
+  const auto weights = [&](const f32x4 (&sc)[RT][2], uint32_t key0, bool edge, auto &&c, typename P::eight (&p)[RT]) {
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      f32x4 sc[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        sc[h] = f32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int j = 0; j < KW; ++j) {
-          if constexpr (E4M3) {
-            sc[h] = product<T>(widen<T>(u32x2{kw[h][j][0], kw[h][j][1]}), q[t][2 * j], sc[h]);
-            sc[h] = product<T>(widen<T>(u32x2{kw[h][j][2], kw[h][j][3]}), q[t][2 * j + 1], sc[h]);
-          } else {
-            sc[h] = product<T>(__builtin_bit_cast(typename T::eight, kw[h][j]), q[t][j], sc[h]);
-          }
-        }
-      }
       float x[8];
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[4 * h + i] = sc[h][i] * ck[h][i] + cv[h][i];
+        for (int i = 0; i < 4; ++i) x[4 * h + i] = E4M3 ? sc[t][h][i] * c(h, i).f + c(h, i).lg : sc[t][h][i] * a.scale_log2;
       if (edge) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const uint32_t key = key0 + 16 * h + 4 * g + i;
-            if (!there[h][i] || key < lo[t] || key >= hi[t]) x[4 * h + i] = -__builtin_inff();
+            if (!c(h, i).ok || key < lo[t] || key >= hi[t]) x[4 * h + i] = -__builtin_inff();
           }
       }
       float top = x[0];
@@ -435,40 +345,49 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(const AttendArgs a) {
         for (int n = 0; n < N; ++n) o[t][n] *= by;
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float w = __builtin_amdgcn_exp2f(x[i] - m[t]);
-        l[t] += E4M3 ? w * iv[i / 4][i % 4] : w;
-        p[t][i] = static_cast<typename P::one>(w);
-      }
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float w = __builtin_amdgcn_exp2f(x[4 * h + i] - m[t]);
+          l[t] += E4M3 ? w * c(h, i).rc : w;
+          p[t][4 * h + i] = static_cast<typename P::one>(w);
+        }
     }
-    // an infinity or NaN that some rows see and others do not: 0 times it is not 0.  It stays out of the products and is
-    // added to the rows that see it (its weight is positive, so what it adds is itself)
+  };
+  // O^T += V^T P^T of a tile
+  const auto values = [&](VWords (&vw)[8], uint32_t key0, bool edge, auto &&c, const typename P::eight (&p)[RT]) {
     bool odd = false;
     if (edge) {
+      // values of keys that no row sees are whatever lies there: nothing of them may reach a product, not even times 0.  An infinity
+      // or NaN that some rows see and others do not stays out of the products too and is added to the rows that see it (its weight is
+      // positive, so what it adds is itself).
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t key = key0 + 16 * (i / 4) + 4 * g + i % 4;
+        if (!c(i / 4, i % 4).ok || key < any_lo || key >= any_hi) vw[i] = VWords{};
 #pragma unroll
-        for (int c = 0; c < VW; ++c) {
-          uint32_t w = word<VW>(vw[i], c);
+        for (int x = 0; x < VW; ++x) {
+          uint32_t w = word<VW>(vw[i], x);
           odd |= without_not_finite<T, E4M3>(w);
-          set_word<VW>(vw[i], c, w);
+          set_word<VW>(vw[i], x, w);
         }
+      }
       odd = __ballot(odd) != 0;
     }
-    // O^T += V^T P^T, 16 values at a time: value n of the lane's, of its eight keys
+    // 16 values at a time: value n of the lane's, of its eight keys
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       u32x4 w;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const uint32_t x = word<VW>(vw[2 * c], E4M3 ? n / 4 : n / 2), y = word<VW>(vw[2 * c + 1], E4M3 ? n / 4 : n / 2);
+      for (int x = 0; x < 4; ++x) {
+        const uint32_t even = word<VW>(vw[2 * x], E4M3 ? n / 4 : n / 2), uneven = word<VW>(vw[2 * x + 1], E4M3 ? n / 4 : n / 2);
         if constexpr (E4M3) {
-          const uint32_t pair = __builtin_amdgcn_perm(y, x, (n & 2) ? 0x07030602u : 0x05010400u);
+          const uint32_t pair = __builtin_amdgcn_perm(uneven, even, (n & 2) ? 0x07030602u : 0x05010400u);
           const f16x2 two = (n & 1) ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(pair, 1.0f, true)
                                     : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(pair, 1.0f, false);
-          w[c] = __builtin_bit_cast(uint32_t, two);
+          w[x] = __builtin_bit_cast(uint32_t, two);
         } else {
-          w[c] = __builtin_amdgcn_perm(y, x, (n & 1) ? 0x07060302u : 0x05040100u);
+          w[x] = __builtin_amdgcn_perm(uneven, even, (n & 1) ? 0x07060302u : 0x05040100u);
         }
       }
       const typename P::eight v = __builtin_bit_cast(typename P::eight, w);
@@ -497,13 +416,150 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(const AttendArgs a) {
         }
       }
     }
+  };
+  const auto load_keys = [&](const uint8_t *at, uint32_t in, u32x4 (&kw)[KW]) {
+#pragma unroll
+    for (int j = 0; j < KW; ++j) {
+      if (!FULL) kw[j] = u32x4{0, 0, 0, 0};
+      if (FULL || j * 64 + g * 16 < a.d * EB) kw[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(at + in + j * 64));
+    }
+  };
+
+  struct Key {
+    float f, lg, rc;  // factor of the score (e4m3); log2 and reciprocal of the value's scale
+    bool ok;
+  };
+  u32x4 kw[2][KW];
+  VWords vw[8];
+  f32x4 sc[RT][2];
+  typename P::eight p[RT];
+  if constexpr (PAGED16) {
+    // A half tile lies in one block.  The halves of the wavefront's next 32 tiles are looked up at once, one to a lane, and come from
+    // there as uniform values.  The keys of the next tile are asked for as soon as the scores of this one have used theirs, its
+    // values as soon as the products have.
+    uint64_t off_l = 0;
+    Key key_l{};
+    uint64_t oks = 0;
+    const uint32_t mine = t1 > t0 + turn ? (t1 - t0 - turn + a.key_waves - 1) / a.key_waves : 0;  // tiles
+    const auto look_up = [&](uint32_t c) {
+      const uint32_t tile = t0 + turn + (c + lane / 2) * a.key_waves, key = tile * kKeyTile + 16 * (lane & 1u);
+      const uint32_t n = block_of(a.pool, key);
+      const uint64_t at = static_cast<uint64_t>(s.table_off) + n;
+      uint32_t id = 0;
+      key_l.ok = tile < t1 && key + 16 > any_lo && key < any_hi;
+      if (key_l.ok) {
+        if (at < a.batch.table_len) id = a.batch.table[at];
+        key_l.ok = at < a.batch.table_len && id < a.pool.num_blocks;
+        if (!key_l.ok) skipped = true;
+      }
+      if (!key_l.ok) id = 0;
+      off_l = id * a.pool.block_stride + head_at + static_cast<uint64_t>(key - n * a.pool.block_tokens) * ts;
+      if constexpr (E4M3) {
+        const float sv = a.pool.v_scale[id * a.pool.scale_stride + kv_head];
+        key_l.f = a.scale_log2 * a.pool.k_scale[id * a.pool.scale_stride + kv_head];
+        key_l.lg = __builtin_amdgcn_logf(sv);
+        key_l.rc = key_l.ok ? 1.0f / sv : 0.0f;
+      }
+      oks = __ballot(key_l.ok);
+    };
+    uint64_t off[2];
+    Key key[2];
+    const auto take = [&](uint32_t c) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t from = (c & 31u) * 2 + h;
+        off[h] = static_cast<uint64_t>(from_lane(static_cast<uint32_t>(off_l >> 32), from)) << 32 | from_lane(static_cast<uint32_t>(off_l), from);
+        key[h].ok = oks >> from & 1u;
+        if constexpr (E4M3) {
+          key[h].f = __uint_as_float(from_lane(__float_as_uint(key_l.f), from));
+          key[h].lg = __uint_as_float(from_lane(__float_as_uint(key_l.lg), from));
+          key[h].rc = __uint_as_float(from_lane(__float_as_uint(key_l.rc), from));
+        }
+      }
+    };
+    const uint32_t k_in = r * ts + (FULL || g * 16 < a.d * EB ? g * 16 : 0);
+    const auto load_values = [&]() {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          vw[4 * h + i] = __builtin_nontemporal_load(reinterpret_cast<const VWords *>(a.pool.v + off[h] + ((4 * g + i) * ts + v_in_row)));
+    };
+    if (mine) {
+      look_up(0);
+      take(0);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) load_keys(a.pool.k + off[h], k_in, kw[h]);
+      load_values();
+    }
+    for (uint32_t c = 0; c < mine; ++c) {
+      const uint32_t key0 = (t0 + turn + c * a.key_waves) * kKeyTile;
+      const Key now[2] = {key[0], key[1]};
+      const bool edge = key0 < all_lo || key0 + kKeyTile > all_hi || !now[0].ok || !now[1].ok;
+      const auto at = [&](int h, int) -> const Key & { return now[h]; };
+      scores(kw, sc);
+      const bool more = c + 1 < mine;
+      if (more) {
+        if (((c + 1) & 31u) == 0) look_up(c + 1);
+        take(c + 1);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) load_keys(a.pool.k + off[h], k_in, kw[h]);
+      }
+      weights(sc, key0, edge, at, p);
+      values(vw, key0, edge, at, p);
+      if (more) load_values();
+    }
+  } else {
+    for (uint32_t tile = t0 + turn; tile < t1; tile += a.key_waves) {
+      const uint32_t key0 = tile * kKeyTile;
+      Key key[2][4];
+      bool edge = key0 < all_lo || key0 + kKeyTile > all_hi;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        // lane r looks up key r of the half; the others' come from it
+        const uint32_t k = key0 + 16 * h + r;
+        const uint32_t n = block_of(a.pool, k);
+        const uint64_t at = static_cast<uint64_t>(s.table_off) + n;
+        uint32_t id = 0;
+        bool ok = k >= any_lo && k < any_hi;
+        if (ok) {
+          if (at < a.batch.table_len) id = a.batch.table[at];
+          ok = at < a.batch.table_len && id < a.pool.num_blocks;
+          if (!ok) skipped = true;
+        }
+        if (__ballot(!ok)) edge = true;
+        if (!ok) id = 0;
+        const uint32_t slot = ok ? k - n * a.pool.block_tokens : 0;
+        Key mine{0, 0, 0, ok};
+        if constexpr (E4M3) {
+          const float sv = a.pool.v_scale[id * a.pool.scale_stride + kv_head];
+          mine.f = a.scale_log2 * a.pool.k_scale[id * a.pool.scale_stride + kv_head];
+          mine.lg = __builtin_amdgcn_logf(sv);
+          mine.rc = ok ? 1.0f / sv : 0.0f;
+        }
+        load_keys(a.pool.k + id * a.pool.block_stride + head_at + static_cast<uint64_t>(slot) * ts, g * 16, kw[h]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int from = static_cast<int>(4 * g + i);
+          const uint32_t id_i = __shfl(id, from, 16), slot_i = __shfl(slot, from, 16);
+          vw[4 * h + i] = *reinterpret_cast<const VWords *>(a.pool.v + id_i * a.pool.block_stride + head_at +
+                                                            static_cast<uint64_t>(slot_i) * ts + v_in_row);
+          key[h][i] = Key{__shfl(mine.f, from, 16), __shfl(mine.lg, from, 16), __shfl(mine.rc, from, 16),
+                          __shfl(static_cast<int>(ok), from, 16) != 0};
+        }
+      }
+      const auto at = [&](int h, int i) -> const Key & { return key[h][i]; };
+      scores(kw, sc);
+      weights(sc, key0, edge, at, p);
+      values(vw, key0, edge, at, p);
+    }
   }
   if (__ballot(skipped) && lane == 0) report(a.status, TUTTI_ST_BAD_BLOCK);
 
-  // the four wavefronts' maxima, sums and rows meet in LDS, 16 rows at a time
+  // the wavefronts' maxima, sums and rows meet in LDS, 16 rows at a time
   constexpr int LD = DP + 4;                        // rows apart by 4 banks
-  __shared__ __attribute__((aligned(16))) float rows[kAttendWaves][16][LD];
-  __shared__ float ml[kAttendWaves][16][2];
+  __shared__ __attribute__((aligned(16))) float rows[kMostWaves][16][LD];
+  __shared__ float ml[kMostWaves][16][2];
   constexpr uint32_t EACH = 8, SEGS = DP / EACH;    // a thread joins 8 values of a row
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
@@ -520,37 +576,37 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(const AttendArgs a) {
         *reinterpret_cast<f32x4 *>(&rows[wave][r][(4 * g + i) * N + n]) =
             f32x4{o[t][n][i], o[t][n + 1][i], o[t][n + 2][i], o[t][n + 3][i]};
     __syncthreads();
-    const uint32_t row_in = threadIdx.x / SEGS, e = (threadIdx.x % SEGS) * EACH, row = row_a + t * 16 + row_in;
-    if (row_in >= 16 || row >= n_rows || e >= a.d) continue;
-    float top = kLowest;
+    for (uint32_t x = threadIdx.x; x < a.abreast * 16 * SEGS; x += blockDim.x) {
+      const uint32_t hw = x / (16 * SEGS), row_in = x / SEGS % 16, e = (x % SEGS) * EACH, row = row_a + t * 16 + row_in;
+      if (row >= n_rows || e >= a.d) continue;
+      float top = kLowest;
+      for (uint32_t w = hw; w < a.abreast * a.key_waves; w += a.abreast) top = fmaxf(top, ml[w][row_in][0]);
+      float sum = 0.0f, y[EACH] = {};
+      for (uint32_t w = hw; w < a.abreast * a.key_waves; w += a.abreast) {
+        const float by = __builtin_amdgcn_exp2f(ml[w][row_in][0] - top);
+        sum += by * ml[w][row_in][1];
 #pragma unroll
-    for (uint32_t w = 0; w < kAttendWaves; ++w) top = fmaxf(top, ml[w][row_in][0]);
-    float sum = 0.0f, y[EACH] = {};
+        for (uint32_t i = 0; i < EACH; ++i) y[i] += by * rows[w][row_in][e + i];
+      }
+      if (u.parts > 1) {
+        const uint64_t at = static_cast<uint64_t>(u.part_slot + hw * u.parts + u.part) * ROWS + t * 16 + row_in;
+        float *to = a.part_o + at * DP + e;
+        *reinterpret_cast<f32x4 *>(to) = f32x4{y[0], y[1], y[2], y[3]};
+        *reinterpret_cast<f32x4 *>(to + 4) = f32x4{y[4], y[5], y[6], y[7]};
+        if (e == 0) a.part_ml[at] = f32x2{top, sum};
+        continue;
+      }
+      const uint32_t i = row / a.group, head = (u.head + hw) * a.group + row - i * a.group;
+      const float by = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+      typename T::eight z;
 #pragma unroll
-    for (uint32_t w = 0; w < kAttendWaves; ++w) {
-      const float by = __builtin_amdgcn_exp2f(ml[w][row_in][0] - top);
-      sum += by * ml[w][row_in][1];
-#pragma unroll
-      for (uint32_t i = 0; i < EACH; ++i) y[i] += by * rows[w][row_in][e + i];
+      for (uint32_t c = 0; c < EACH; ++c) z[c] = static_cast<typename T::one>(y[c] * by);
+      *reinterpret_cast<u32x4 *>(static_cast<uint8_t *>(a.out.base) + static_cast<uint64_t>(s.row0 + i) * a.out.row_stride +
+                                 head * a.out.head_stride + 2 * e) = __builtin_bit_cast(u32x4, z);
+      if (e == 0 && a.lse)
+        a.lse[static_cast<uint64_t>(s.row0 + i) * (a.kv_heads * a.group) + head] =
+            sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * kLn2;
     }
-    if (u.parts > 1) {
-      const uint64_t at = static_cast<uint64_t>(u.part_slot + u.part) * ROWS + t * 16 + row_in;
-      float *to = a.part_o + at * DP + e;
-      *reinterpret_cast<f32x4 *>(to) = f32x4{y[0], y[1], y[2], y[3]};
-      *reinterpret_cast<f32x4 *>(to + 4) = f32x4{y[4], y[5], y[6], y[7]};
-      if (e == 0) a.part_ml[at] = f32x2{top, sum};
-      continue;
-    }
-    const uint32_t i = row / a.group, head = u.head * a.group + row - i * a.group;
-    const float by = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-    typename T::eight z;
-#pragma unroll
-    for (uint32_t c = 0; c < EACH; ++c) z[c] = static_cast<typename T::one>(y[c] * by);
-    *reinterpret_cast<u32x4 *>(static_cast<uint8_t *>(a.out.base) + static_cast<uint64_t>(s.row0 + i) * a.out.row_stride +
-                               head * a.out.head_stride + 2 * e) = __builtin_bit_cast(u32x4, z);
-    if (e == 0 && a.lse)
-      a.lse[static_cast<uint64_t>(s.row0 + i) * (a.kv_heads * a.group) + head] =
-          sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * kLn2;
   }
 }
 
@@ -574,10 +630,10 @@ __global__ __launch_bounds__(256) void k_kv_join(const AttendArgs a) {
       s = load_seq(a.batch.seqs + base + lane);
       if (seq_ok(a.batch, s) && s.n_new) {
         p = parts_of(a, plan, s);
-        all = row_tiles<ROWS>(a, s) * a.kv_heads * p;
+        all = row_tiles<ROWS>(a, s) * (a.kv_heads / a.abreast) * p;
         if (p > 1) {
           n = s.n_new * a.group * a.kv_heads;
-          split = all;
+          split = row_tiles<ROWS>(a, s) * a.kv_heads * p;
         }
       }
     }
