@@ -112,9 +112,10 @@ int turn_of(const RopeView &r) {
 
 // ---- attend
 
-// Rows of queries a workgroup takes: 16 where no sequence has more, else 32.
+// Rows of queries a workgroup takes: 16 or 32 where no sequence has more, else 128 (with keys and values in LDS).
 uint32_t rows_a_tile(const tutti_batch *b, uint32_t group) {
-  return static_cast<uint64_t>(b->max_new) * group <= 16 ? 16 : 32;
+  const uint64_t most = static_cast<uint64_t>(b->max_new) * group;
+  return most <= 16 ? 16 : most <= 32 ? 32 : 128;
 }
 
 // Neighbouring KV heads that a workgroup takes side by side, so that it reads stretches of a block and not a head's rows here and
@@ -136,9 +137,14 @@ int attend_sizes(const tutti_pool *pool, const tutti_batch *b, const tutti_attn 
   const uint32_t group = attn->n_q_heads / pool->num_kv_heads;
   s->rows = rows_a_tile(b, group);
   s->dp = pool->head_dim <= 64 ? 64 : 128;
-  s->abreast = heads_abreast(pool->num_kv_heads);
-  s->key_waves = s->abreast == 1 ? 4 : s->abreast == 2 ? 2 : 1;
-  s->target = 768;  // three workgroups a compute unit: what fits of most kernels
+  if (s->rows < 128) {
+    s->abreast = heads_abreast(pool->num_kv_heads);
+    s->key_waves = s->abreast == 1 ? 4 : s->abreast == 2 ? 2 : 1;
+    s->target = 768;  // three workgroups a compute unit: what fits of most kernels
+  } else {
+    s->abreast = s->key_waves = 1;
+    s->target = 512;
+  }
   const uint64_t tiles = static_cast<uint64_t>(b->n_rows) * group / s->rows + std::min(b->n_seq, b->n_rows);
   const uint64_t units = s->target + tiles * (pool->num_kv_heads / s->abreast);
   if (units >= 0x80000000ull || static_cast<uint64_t>(b->n_rows) * attn->n_q_heads >= 0x80000000ull) return TUTTI_ERANGE;
@@ -174,8 +180,37 @@ void launch_join(const AttendArgs &a, hipStream_t stream) {
   else
     hipLaunchKernelGGL((k_kv_join<T, DP, ROWS, 1>), dim3((joins + 3) / 4), dim3(256), 0, stream, a);
 }
+template <typename T, bool E4M3, bool PAGED16>
+void launch_wide(const AttendArgs &a, hipStream_t stream) {
+  const dim3 grid(a.max_units), wg(256);
+  if (a.d == 128)
+    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 128, true, PAGED16, 1>), grid, wg, 0, stream, a);
+  else if (a.d == 112)
+    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 112, true, PAGED16, 1>), grid, wg, 0, stream, a);
+  else if (a.d == 96)
+    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 96, true, PAGED16, 1>), grid, wg, 0, stream, a);
+  else if (a.d == 80)
+    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 80, true, PAGED16, 1>), grid, wg, 0, stream, a);
+  else if (a.d == 64)
+    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 64, true, PAGED16, 1>), grid, wg, 0, stream, a);
+  else
+    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 64, false, PAGED16, 1>), grid, wg, 0, stream, a);
+}
 template <typename T, bool E4M3, int DP>
 void launch_attend(const AttendArgs &a, uint32_t rows, hipStream_t stream) {
+  if (rows == 128) {
+    // (keys are looked up one by one whatever the block's size; e4m3 scales of 16 keys at a time where they are one block's)
+    if constexpr (E4M3) {
+      if (a.pool.block_tokens % 16 == 0)
+        launch_wide<T, true, true>(a, stream);
+      else
+        launch_wide<T, true, false>(a, stream);
+    } else {
+      launch_wide<T, false, true>(a, stream);
+    }
+    launch_join<T, DP, 128>(a, stream);
+    return;
+  }
   if (a.pool.block_tokens % 16 == 0)
     rows == 16 ? launch_attend<T, E4M3, DP, true, 1>(a, stream) : launch_attend<T, E4M3, DP, true, 2>(a, stream);
   else

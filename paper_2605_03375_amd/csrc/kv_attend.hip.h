@@ -395,7 +395,8 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 ? 3 : 2) void k_kv_attend(
       for (int t = 0; t < RT; ++t) o[t][n] = product<P>(v, p[t], o[t][n]);
     }
     if (odd) {
-      for (uint32_t key = max(key0, any_lo); key < min(key0 + kKeyTile, any_hi); ++key) {
+      const uint32_t from = key0 > any_lo ? key0 : any_lo, to = key0 + kKeyTile < any_hi ? key0 + kKeyTile : any_hi;
+      for (uint32_t key = from; key < to; ++key) {
         const uint32_t n = block_of(a.pool, key);
         const uint64_t at = static_cast<uint64_t>(s.table_off) + n;
         const uint32_t id = at < a.batch.table_len ? a.batch.table[at] : ~0u;
@@ -607,6 +608,488 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 ? 3 : 2) void k_kv_attend(
         a.lse[static_cast<uint64_t>(s.row0 + i) * (a.kv_heads * a.group) + head] =
             sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * kLn2;
     }
+  }
+}
+
+// ---- Many queries: a workgroup of four wavefronts takes 128*RW rows of queries, a KV head and a part of the keys, 64 at a time.
+//
+// A tile of keys and values lies in LDS as 16-bit rows, twice: while one is worked on the next is on its way (16-bit blocks straight
+// from memory to LDS, e4m3 through registers, where it is widened).  Units of 16 bytes are swapped within a row by the row's number, so
+// that neither the keys' rows nor the transposed reads of the values meet in a bank; the swap is made by which address a lane
+// loads.  S^T = K Q^T and O^T = V^T P^T with 32x32x16 matrix instructions: lane (r = l % 32, h = l / 32) holds row r of the queries
+// and keys 8i+4h..8i+4h+3 of each 32, and the weights go from one product to the other where they are; values are read
+// transposed, four keys of 16 values at a time.
+constexpr uint32_t kWideTile = 64;
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+#define TUTTI_LDS __attribute__((address_space(3)))
+#define TUTTI_GLOBAL __attribute__((address_space(1)))
+
+template <typename T>
+__device__ __forceinline__ f32x16 wide_product(typename T::eight a, typename T::eight b, f32x16 c) {
+  if constexpr (__is_same(T, Fp16))
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+__device__ __forceinline__ float max_of_halves(float x) {
+  const uint32_t a = __float_as_uint(x);
+  const auto q = __builtin_amdgcn_permlane32_swap(a, a, false, false);
+  return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
+__device__ __forceinline__ float sum_of_halves(float x) {
+  const uint32_t a = __float_as_uint(x);
+  const auto q = __builtin_amdgcn_permlane32_swap(a, a, false, false);
+  return __uint_as_float(q[0]) + __uint_as_float(q[1]);
+}
+
+// D: values of a head that it is built for; FULL: a head has so many (else fewer than 64, and D is 64).
+template <typename T, bool E4M3, int D, bool FULL, bool PAGED16, int RW>
+__global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const AttendArgs a) {
+  constexpr int DP = D <= 64 ? 64 : 128, ROWS = 128 * RW, STEPS = D / 16, DT = (D + 31) / 32;
+  constexpr uint32_t UNITS = DP / 8, ROW_BYTES = DP * 2, PLANE = kWideTile * ROW_BYTES, BUFFER = 2 * PLANE;
+  constexpr uint32_t EB = E4M3 ? 1 : 2;
+  using P = std::conditional_t<E4M3, Fp16, T>;
+  const uint32_t d = FULL ? D : a.d;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * BUFFER];
+  __shared__ float per_key[E4M3 && !PAGED16 ? 4 : 1][3][kWideTile];
+
+  const uint32_t lane = threadIdx.x & (kLanes - 1), wave = uniform(threadIdx.x / kLanes);
+  const uint32_t r = lane & 31u, hf = lane >> 5;
+  const bool reporter = blockIdx.x == 0 && wave == 0;
+  if (blockIdx.x >= a.max_units) return;
+  const Plan plan = make_plan<ROWS>(a);
+  const Unit u = locate<ROWS>(a, plan, blockIdx.x, reporter);
+  if (u.seq == a.batch.n_seq) return;
+  if (u.parts > 1 && u.part_slot + u.parts > a.max_parts) {
+    if (threadIdx.x == 0) report(a.status, TUTTI_ST_BAD_EXTENT);
+    return;
+  }
+  const tutti_seq s = u.s;
+  const uint32_t begin = s.n_held - s.n_new, n_rows = s.n_new * a.group;
+
+  // the keys that a place sees: [low(place), high(place))
+  const auto high = [&](uint32_t place) { return a.causal ? place + 1 : s.n_held; };
+  const auto low = [&](uint32_t place) { return a.window && place + 1 > a.window ? place + 1 - a.window : 0; };
+  // those that any row, and that all rows, of the workgroup (of the wavefront) see
+  const uint32_t row_a = u.row_tile * ROWS, row_b = min(row_a + ROWS, n_rows) - 1;
+  const uint32_t place_a = begin + row_a / a.group, place_b = begin + row_b / a.group;
+  const uint32_t any_lo = uniform(low(place_a)), any_hi = uniform(high(place_b)), all_lo = uniform(low(place_b)), all_hi = uniform(high(place_a));
+  const uint32_t wave_a = row_a + wave * 32 * RW, wave_b = min(wave_a + 32 * RW, n_rows);
+  const bool has_rows = wave_a < wave_b;
+  const uint32_t w_place_a = has_rows ? begin + wave_a / a.group : 0, w_place_b = has_rows ? begin + (wave_b - 1) / a.group : 0;
+  const uint32_t w_any_lo = uniform(low(w_place_a)), w_any_hi = has_rows ? uniform(high(w_place_b)) : 0;
+  const uint32_t w_all_lo = uniform(low(w_place_b)), w_all_hi = uniform(high(w_place_a));
+  const uint32_t tile_lo = any_lo / kWideTile, tiles = (any_hi + kWideTile - 1) / kWideTile - tile_lo;
+  const uint32_t t0 = uniform(tile_lo + static_cast<uint32_t>(static_cast<uint64_t>(tiles) * u.part / u.parts));
+  const uint32_t t1 = uniform(tile_lo + static_cast<uint32_t>(static_cast<uint64_t>(tiles) * (u.part + 1) / u.parts));
+
+  uint32_t lo[RW], hi[RW];
+  typename T::eight q[RW][STEPS];
+  const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0;  // scores are multiplied by a factor that is positive
+  const float factor = fmaxf(fabsf(a.scale_log2), 0x1p-100f);   // (0: no score counts; times 0, a masked one would be no number)
+#pragma unroll
+  for (int t = 0; t < RW; ++t) {
+    const uint32_t row = wave_a + t * 32 + r;
+    const bool in = row < n_rows;
+    const uint32_t i = in ? row / a.group : 0, head = u.head * a.group + (in ? row - i * a.group : 0);
+    hi[t] = high(begin + i);
+    lo[t] = low(begin + i);
+    const uint8_t *at = static_cast<const uint8_t *>(a.q.base) + static_cast<uint64_t>(s.row0 + i) * a.q.row_stride + head * a.q.head_stride;
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j) {
+      u32x4 w = {0, 0, 0, 0};
+      if (FULL || j * 16 < static_cast<int>(d)) w = *reinterpret_cast<const u32x4 *>(at + j * 32 + hf * 16);
+      w ^= u32x4{flip, flip, flip, flip};
+      q[t][j] = __builtin_bit_cast(typename T::eight, w);
+    }
+  }
+  f32x16 o[RW][DT];
+  float m[RW], l[RW];
+#pragma unroll
+  for (int t = 0; t < RW; ++t) {
+    m[t] = kLowest;
+    l[t] = 0.0f;
+#pragma unroll
+    for (int n = 0; n < DT; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[t][n][i] = 0.0f;
+  }
+
+  const uint64_t head_at = static_cast<uint64_t>(u.head) * a.pool.head_stride;
+  const uint32_t ts = a.pool.token_stride;
+  TUTTI_LDS uint8_t *const base = (TUTTI_LDS uint8_t *)lds;
+  if (!FULL || D != DP) {  // units behind the rows' ends are never written: what lies there meets weights
+    for (uint32_t x = threadIdx.x * 16; x < 2 * BUFFER; x += 256 * 16) *(TUTTI_LDS u32x4 *)(base + x) = u32x4{0, 0, 0, 0};
+    __syncthreads();
+  }
+
+  // a tile's blocks, one key to a lane
+  bool skipped = false;
+  uint32_t id_next = 0;
+  bool ok_next = false;
+  const auto look_up = [&](uint32_t tile) {
+    const uint32_t key = tile * kWideTile + lane;
+    const uint64_t at = static_cast<uint64_t>(s.table_off) + block_of(a.pool, key);
+    ok_next = tile < t1 && key >= any_lo && key < any_hi;
+    id_next = 0;
+    if (ok_next) {
+      if (at < a.batch.table_len)
+        id_next = a.batch.table[at];
+      else
+        id_next = ~0u;
+    }
+  };
+  struct Tile {
+    uint64_t oks;
+    float f[4], lg[4], rc[4];  // PAGED16: of each 16 keys
+  };
+  Tile next{}, now{};
+  u32x4 raw[E4M3 ? DP / 32 : 1];
+  constexpr uint32_t CHUNKS = kWideTile * DP * EB / 4096;   // 1 KiB each, of a plane, that a wavefront brings
+  constexpr uint32_t LANES_A_ROW = DP * EB / 16, ROWS_A_CHUNK = kLanes / LANES_A_ROW;
+  // asks for what look_up() has found
+  const auto fetch = [&](uint32_t tile, uint32_t buffer) {
+    const uint32_t key = tile * kWideTile + lane;
+    if (ok_next && id_next >= a.pool.num_blocks) {
+      ok_next = false;
+      skipped = true;
+    }
+    const uint32_t id = ok_next ? id_next : 0, slot = key - block_of(a.pool, key) * a.pool.block_tokens;
+    const uint64_t off = id * a.pool.block_stride + head_at + static_cast<uint64_t>(slot) * ts;
+    next.oks = __ballot(ok_next);
+    if constexpr (E4M3) {
+      const float sv = a.pool.v_scale[id * a.pool.scale_stride + u.head];
+      // (not 0: times 0, a score of -infinity would be no number)
+      const float f = ok_next ? fmaxf(factor * a.pool.k_scale[id * a.pool.scale_stride + u.head], 0x1p-120f) : 1.0f;
+      const float lg = ok_next ? __builtin_amdgcn_logf(sv) : 0.0f, rc = ok_next ? 1.0f / sv : 0.0f;
+      if constexpr (PAGED16) {
+        // (a key that is not there may stand in front of one that is: the last of its 16 that is there speaks for all)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const uint32_t some = static_cast<uint32_t>(next.oks >> (16 * x)) & 0xffffu;
+          const uint32_t from = 16 * x + (some ? 31 - __builtin_clz(some) : 0);
+          next.f[x] = __uint_as_float(from_lane(__float_as_uint(f), from));
+          next.lg[x] = __uint_as_float(from_lane(__float_as_uint(lg), from));
+          next.rc[x] = __uint_as_float(from_lane(__float_as_uint(rc), from));
+        }
+      } else {
+        next.f[0] = f;   // per lane: to LDS when the tile's turn comes
+        next.lg[0] = lg;
+        next.rc[0] = rc;
+      }
+    }
+#pragma unroll
+    for (uint32_t c = 0; c < CHUNKS; ++c) {
+      const uint32_t row = (wave * CHUNKS + c) * ROWS_A_CHUNK + lane / LANES_A_ROW, place = lane % LANES_A_ROW;
+      const uint64_t from = static_cast<uint64_t>(__shfl(static_cast<uint32_t>(off >> 32), row, kLanes)) << 32 |
+                            __shfl(static_cast<uint32_t>(off), row, kLanes);
+      if constexpr (E4M3) {
+        const bool in = place * 16 < d;
+        const bool ok = next.oks >> row & 1u;
+        raw[c] = raw[CHUNKS + c] = u32x4{0, 0, 0, 0};
+        if (in && ok) {
+          raw[c] = *reinterpret_cast<const u32x4 *>(a.pool.k + from + place * 16);
+          raw[CHUNKS + c] = *reinterpret_cast<const u32x4 *>(a.pool.v + from + place * 16);
+        }
+      } else {
+        const uint32_t unit = place ^ (row & (UNITS - 1));
+        if (unit * 8 < d) {
+          TUTTI_LDS uint8_t *to = base + buffer * BUFFER + (wave * CHUNKS + c) * 1024;
+          __builtin_amdgcn_global_load_lds((const TUTTI_GLOBAL void *)(a.pool.k + from + unit * 16), (TUTTI_LDS void *)to, 16, 0, 0);
+          __builtin_amdgcn_global_load_lds((const TUTTI_GLOBAL void *)(a.pool.v + from + unit * 16), (TUTTI_LDS void *)(to + PLANE), 16, 0, 0);
+        }
+      }
+    }
+  };
+  // e4m3: widens what fetch() has brought
+  const auto put = [&](uint32_t buffer) {
+    if constexpr (E4M3) {
+#pragma unroll
+      for (uint32_t c = 0; c < 2 * CHUNKS; ++c) {
+        const bool value = c >= CHUNKS;
+        const uint32_t row = (wave * CHUNKS + c % CHUNKS) * ROWS_A_CHUNK + lane / LANES_A_ROW, place = lane % LANES_A_ROW;
+        TUTTI_LDS uint8_t *to = base + buffer * BUFFER + (value ? PLANE : 0) + row * ROW_BYTES;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const u32x2 codes = {raw[c][2 * x], raw[c][2 * x + 1]};
+          const uint32_t unit = (2 * place + x) ^ (row & (UNITS - 1));
+          u32x4 w;
+          if (value)
+            w = __builtin_bit_cast(u32x4, widen<Fp16>(codes));
+          else
+            w = __builtin_bit_cast(u32x4, widen<T>(codes));
+          *(TUTTI_LDS u32x4 *)(to + unit * 16) = w;
+        }
+      }
+    }
+  };
+
+  // where a lane reads: keys, per step of 16 values; values, per exclusive-or of their unit
+  uint32_t key_at[STEPS], value_at[4];
+#pragma unroll
+  for (int j = 0; j < STEPS; ++j) key_at[j] = r * ROW_BYTES + ((2 * j + hf) ^ (r & (UNITS - 1))) * 16;
+  {
+    const uint32_t j = lane & 15u, grp = lane >> 4, row = 4 * (grp >> 1) + j / 4;
+    const uint32_t unit = (2 * (grp & 1u) + (j & 3u) / 2) ^ row;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) value_at[x] = PLANE + row * ROW_BYTES + (unit ^ (x << 2)) * 16 + (j & 1u) * 8;
+  }
+
+  // keys 16x.. of the tile, values 32n..: what the products take
+  const auto values_of = [&](TUTTI_LDS uint8_t *from, int n, int x) {
+    s16x4 v[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+      v[c] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (TUTTI_LDS s16x4 *)(from + value_at[DP == 128 ? n ^ (2 * c) : n] + (16 * x + 8 * c) * ROW_BYTES));
+    return __builtin_bit_cast(typename P::eight, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+
+  if (t1 > t0) {
+    look_up(t0);
+    fetch(t0, 0);
+    look_up(t0 + 1);
+    put(0);
+  }
+  for (uint32_t tile = t0; tile < t1; ++tile) {
+    const uint32_t buffer = (tile - t0) & 1u, key0 = tile * kWideTile;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    now = next;
+    const bool more = tile + 1 < t1;
+    if (E4M3 && !PAGED16) {
+      per_key[wave][0][lane] = now.f[0];
+      per_key[wave][1][lane] = now.lg[0];
+      per_key[wave][2][lane] = now.rc[0];
+    }
+    if (more) {
+      fetch(tile + 1, buffer ^ 1u);
+      look_up(tile + 2);
+    }
+    TUTTI_LDS uint8_t *const here = base + buffer * BUFFER;
+    const bool wg_edge = key0 < all_lo || key0 + kWideTile > all_hi || now.oks != ~0ull;
+    bool odd = false;
+    if (wg_edge) {
+      // values of keys that no row sees are whatever lies there, and an infinity or NaN that some rows see must not meet the others'
+      // weights of 0: both leave the tile, the latter are added to the rows that see them further down
+      constexpr uint32_t EACH = PLANE / 256 / 16;
+      bool any = false;
+#pragma unroll
+      for (uint32_t x = 0; x < EACH; ++x) {
+        const uint32_t unit = threadIdx.x * EACH + x, row = unit / UNITS;
+        TUTTI_LDS u32x4 *at = (TUTTI_LDS u32x4 *)(here + PLANE + unit * 16);
+        u32x4 w = *at;
+        if (!(now.oks >> row & 1u)) w = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t one = w[c];
+          any |= without_not_finite<P, false>(one);
+          w[c] = one;
+        }
+        *at = w;
+      }
+      odd = __syncthreads_or(any);
+    }
+    if (has_rows && key0 < w_any_hi && key0 + kWideTile > w_any_lo) {
+      const bool edge = key0 < w_all_lo || key0 + kWideTile > w_all_hi || now.oks != ~0ull;
+      typename P::eight p[RW][4];
+      f32x16 sc[RW][2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int t = 0; t < RW; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sc[t][h][i] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < STEPS; ++j) {
+          const typename T::eight k = __builtin_bit_cast(typename T::eight, *(TUTTI_LDS u32x4 *)(here + key_at[j] + h * 32 * ROW_BYTES));
+#pragma unroll
+          for (int t = 0; t < RW; ++t) sc[t][h] = wide_product<T>(k, q[t][j], sc[t][h]);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < RW; ++t) {
+        if (E4M3 && !PAGED16) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+              const f32x4 f = *reinterpret_cast<const f32x4 *>(&per_key[wave][0][32 * h + 2 * i + 4 * hf]);
+              const f32x4 lg = *reinterpret_cast<const f32x4 *>(&per_key[wave][1][32 * h + 2 * i + 4 * hf]);
+#pragma unroll
+              for (int x = 0; x < 4; ++x) sc[t][h][i + x] = sc[t][h][i + x] * f[x] + lg[x];
+            }
+        }
+        if (edge) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const uint32_t in = 32 * h + 8 * (i / 4) + 4 * hf + i % 4, key = key0 + in;
+              if (!(now.oks >> in & 1u) || key < lo[t] || key >= hi[t]) sc[t][h][i] = -__builtin_inff();
+            }
+        }
+        // the largest of each 16 keys, then with their factors of all
+        float top = kLowest;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          float most = sc[t][x / 2][8 * (x & 1)];
+#pragma unroll
+          for (int i = 1; i < 8; ++i) most = fmaxf(most, sc[t][x / 2][8 * (x & 1) + i]);
+          if constexpr (E4M3 && PAGED16) most = most * now.f[x] + now.lg[x];
+          top = fmaxf(top, most);
+        }
+        if (!E4M3) top *= factor;
+        top = max_of_halves(top);
+        if (__ballot(top > m[t] + kRaise)) {
+          const float raised = top > m[t] + kRaise ? top : m[t];
+          const float by = __builtin_amdgcn_exp2f(m[t] - raised);
+          m[t] = raised;
+          l[t] *= by;
+#pragma unroll
+          for (int n = 0; n < DT; ++n) o[t][n] *= by;
+        }
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const float f = E4M3 ? (PAGED16 ? now.f[x] : 1.0f) : factor, less = (E4M3 && PAGED16 ? now.lg[x] : 0.0f) - m[t];
+          float sum = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][x / 2][8 * (x & 1) + i], f, less));
+            if constexpr (E4M3 && !PAGED16)
+              sum += w * per_key[wave][2][16 * x + 8 * (i / 4) + 4 * hf + i % 4];
+            else
+              sum += w;
+            p[t][x][i] = static_cast<typename P::one>(w);
+          }
+          l[t] += E4M3 && PAGED16 ? sum * now.rc[x] : sum;
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int n = 0; n < DT; ++n) {
+          const typename P::eight both = values_of(here, n, x);
+#pragma unroll
+          for (int t = 0; t < RW; ++t) o[t][n] = wide_product<P>(both, p[t][x], o[t][n]);
+        }
+    }
+    if (odd) {
+      // the infinities and NaN of the tile as numbers that say what they are, for the rows that see them: 1, 2^7 and 2^14, sums of
+      // 64 of which say which there were
+      __syncthreads();
+#pragma unroll 1
+      for (uint32_t x = threadIdx.x; x < PLANE / 16; x += 256) {
+        const uint32_t row = x / UNITS, d0 = ((x % UNITS) ^ (row & (UNITS - 1))) * 8, key = key0 + row;
+        typename P::eight w = {};
+        if (d0 < d && key >= any_lo && key < any_hi) {
+          const uint32_t n = block_of(a.pool, key);
+          const uint64_t at = static_cast<uint64_t>(s.table_off) + n;
+          const uint32_t id = at < a.batch.table_len ? a.batch.table[at] : ~0u;
+          if (id < a.pool.num_blocks) {
+            const uint8_t *from = a.pool.v + id * a.pool.block_stride + head_at + static_cast<uint64_t>(key - n * a.pool.block_tokens) * ts;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+              const float e = element<T, E4M3>(from, d0 + c);
+              w[c] = static_cast<typename P::one>(e != e ? 16384.0f : e == __builtin_inff() ? 1.0f : e == -__builtin_inff() ? 128.0f : 0.0f);
+            }
+          }
+        }
+        *(TUTTI_LDS u32x4 *)(here + PLANE + x * 16) = __builtin_bit_cast(u32x4, w);
+      }
+      __syncthreads();
+      if (has_rows) {
+#pragma unroll
+        for (int n = 0; n < DT; ++n) {
+          f32x16 sums[RW];
+#pragma unroll
+          for (int t = 0; t < RW; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sums[t][i] = 0.0f;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const typename P::eight v = values_of(here, n, x);
+#pragma unroll
+            for (int t = 0; t < RW; ++t) {
+              typename P::eight seen;
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const uint32_t key = key0 + 16 * x + 8 * (i / 4) + 4 * hf + i % 4;
+                seen[i] = static_cast<typename P::one>(key >= lo[t] && key < hi[t] ? 1.0f : 0.0f);
+              }
+              sums[t] = wide_product<P>(v, seen, sums[t]);
+            }
+          }
+#pragma unroll
+          for (int t = 0; t < RW; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const uint32_t which = static_cast<uint32_t>(sums[t][i]);
+              const bool up = which & 0x7fu, down = which >> 7 & 0x7fu, none = which >> 14;
+              if (which) o[t][n][i] += none || (up && down) ? __builtin_nanf("") : up ? __builtin_inff() : -__builtin_inff();
+            }
+        }
+      }
+    }
+    if (more) put(buffer ^ 1u);
+  }
+  if (__ballot(skipped) && lane == 0) report(a.status, TUTTI_ST_BAD_BLOCK);
+  __syncthreads();  // LDS changes hands: from here each wavefront has a part of it
+  const AttendArgs &z = arguments_again<AttendArgs>();
+
+#pragma unroll
+  for (int t = 0; t < RW; ++t) {
+    const float sum = sum_of_halves(l[t]);
+    const uint32_t row_in = wave * 32 * RW + t * 32 + r, row = row_a + row_in;
+    if (u.parts > 1) {
+      if (row < n_rows) {
+        const uint64_t at = static_cast<uint64_t>(u.part_slot + u.part) * ROWS + row_in;
+#pragma unroll
+        for (int n = 0; n < DT; ++n)
+#pragma unroll
+          for (int i = 0; i < 16; i += 4)
+            *reinterpret_cast<f32x4 *>(z.part_o + at * DP + 32 * n + 2 * i + 4 * hf) =
+                f32x4{o[t][n][i], o[t][n][i + 1], o[t][n][i + 2], o[t][n][i + 3]};
+        if (hf == 0) z.part_ml[at] = f32x2{m[t], sum};
+      }
+      continue;
+    }
+    // through LDS, so that whole rows are stored
+    constexpr uint32_t OUT_BYTES = ROW_BYTES + 16;
+    TUTTI_LDS uint8_t *const mine = base + wave * 32 * OUT_BYTES;
+    const float by = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+#pragma unroll
+    for (int n = 0; n < DT; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        typename T::two two[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          two[x][0] = static_cast<typename T::one>(o[t][n][i + 2 * x] * by);
+          two[x][1] = static_cast<typename T::one>(o[t][n][i + 2 * x + 1] * by);
+        }
+        *(TUTTI_LDS u32x2 *)(mine + r * OUT_BYTES + (32 * n + 2 * i + 4 * hf) * 2) =
+            u32x2{__builtin_bit_cast(uint32_t, two[0]), __builtin_bit_cast(uint32_t, two[1])};
+      }
+    if (row < n_rows && hf == 0 && z.lse) {
+      const uint32_t i = row / z.group, head = u.head * z.group + row - i * z.group;
+      z.lse[static_cast<uint64_t>(s.row0 + i) * (z.kv_heads * z.group) + head] =
+          sum == 0.0f ? -__builtin_inff() : (m[t] + __builtin_amdgcn_logf(sum)) * kLn2;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    for (uint32_t x = lane; x < 32 * UNITS; x += kLanes) {
+      const uint32_t in = x / UNITS, unit = x % UNITS, out_row = wave_a + t * 32 + in;
+      if (out_row >= n_rows || unit * 8 >= d) continue;
+      const uint32_t i = out_row / z.group, head = u.head * z.group + out_row - i * z.group;
+      *reinterpret_cast<u32x4 *>(static_cast<uint8_t *>(z.out.base) + static_cast<uint64_t>(s.row0 + i) * z.out.row_stride +
+                                 head * z.out.head_stride + unit * 16) = *(TUTTI_LDS u32x4 *)(mine + in * OUT_BYTES + unit * 16);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
