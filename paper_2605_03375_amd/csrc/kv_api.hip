@@ -199,15 +199,10 @@ void launch_wide(const AttendArgs &a, hipStream_t stream) {
 template <typename T, bool E4M3, int DP>
 void launch_attend(const AttendArgs &a, uint32_t rows, hipStream_t stream) {
   if (rows == 128) {
-    // (keys are looked up one by one whatever the block's size; e4m3 scales of 16 keys at a time where they are one block's)
-    if constexpr (E4M3) {
-      if (a.pool.block_tokens % 16 == 0)
-        launch_wide<T, true, true>(a, stream);
-      else
-        launch_wide<T, true, false>(a, stream);
-    } else {
-      launch_wide<T, false, true>(a, stream);
-    }
+    if (a.pool.block_tokens % 16 == 0)
+      launch_wide<T, E4M3, true>(a, stream);
+    else
+      launch_wide<T, E4M3, false>(a, stream);
     launch_join<T, DP, 128>(a, stream);
     return;
   }

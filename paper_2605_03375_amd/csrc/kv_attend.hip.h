@@ -324,6 +324,7 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 ? 3 : 2) void k_kv_attend(
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[4 * h + i] = E4M3 ? sc[t][h][i] * c(h, i).f + c(h, i).lg : sc[t][h][i] * a.scale_log2;
       if (edge) {
+        asm volatile("" ::);  // (a branch: most tiles are whole ones)
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -358,6 +359,7 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 ? 3 : 2) void k_kv_attend(
   const auto values = [&](VWords (&vw)[8], uint32_t key0, bool edge, auto &&c, const typename P::eight (&p)[RT]) {
     bool odd = false;
     if (edge) {
+      asm volatile("" ::);
       // values of keys that no row sees are whatever lies there: nothing of them may reach a product, not even times 0.  An infinity
       // or NaN that some rows see and others do not stays out of the products too and is added to the rows that see it (its weight is
       // positive, so what it adds is itself).
@@ -459,7 +461,7 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 ? 3 : 2) void k_kv_attend(
         const float sv = a.pool.v_scale[id * a.pool.scale_stride + kv_head];
         key_l.f = a.scale_log2 * a.pool.k_scale[id * a.pool.scale_stride + kv_head];
         key_l.lg = __builtin_amdgcn_logf(sv);
-        key_l.rc = key_l.ok ? 1.0f / sv : 0.0f;
+        key_l.rc = key_l.ok ? __builtin_amdgcn_rcpf(sv) : 0.0f;
       }
       oks = __ballot(key_l.ok);
     };
@@ -536,7 +538,7 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 ? 3 : 2) void k_kv_attend(
           const float sv = a.pool.v_scale[id * a.pool.scale_stride + kv_head];
           mine.f = a.scale_log2 * a.pool.k_scale[id * a.pool.scale_stride + kv_head];
           mine.lg = __builtin_amdgcn_logf(sv);
-          mine.rc = ok ? 1.0f / sv : 0.0f;
+          mine.rc = ok ? __builtin_amdgcn_rcpf(sv) : 0.0f;
         }
         load_keys(a.pool.k + id * a.pool.block_stride + head_at + static_cast<uint64_t>(slot) * ts, g * 16, kw[h]);
 #pragma unroll
@@ -615,8 +617,8 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 ? 3 : 2) void k_kv_attend(
 //
 // A tile of keys and values lies in LDS as 16-bit rows, twice: while one is worked on the next is on its way (16-bit blocks straight
 // from memory to LDS, e4m3 through registers, where it is widened).  Units of 16 bytes are swapped within a row by the row's number, so
-// that neither the keys' rows nor the transposed reads of the values meet in a bank; the swap is made by which address a lane
-// loads.  S^T = K Q^T and O^T = V^T P^T with 32x32x16 matrix instructions: lane (r = l % 32, h = l / 32) holds row r of the queries
+// that neither 16 keys' rows nor the transposed reads of four values' rows meet in one of the 64 banks; the swap is made by which
+// address a lane loads.  S^T = K Q^T and O^T = V^T P^T with 32x32x16 matrix instructions: lane (r = l % 32, h = l / 32) holds row r of the queries
 // and keys 8i+4h..8i+4h+3 of each 32, and the weights go from one product to the other where they are; values are read
 // transposed, four keys of 16 values at a time.
 constexpr uint32_t kWideTile = 64;
@@ -625,6 +627,19 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 #define TUTTI_LDS __attribute__((address_space(3)))
 #define TUTTI_GLOBAL __attribute__((address_space(1)))
+
+// What the number of a unit of a row is exclusive-ored with.  Rows of 16 units: four rows lie in four quarters of the banks, 16 rows' same
+// unit in all of them; rows of 8 units: the same, two rows to a round of the banks.
+template <int UNITS>
+__device__ __forceinline__ uint32_t swap_of(uint32_t row) {
+  return UNITS == 16 ? (row & 3u) << 2 | (row >> 2 & 3u) : (row >> 1 & 1u) << 2 | (row >> 2 & 3u);
+}
+
+// LDS by its address there.
+template <typename E>
+__device__ __forceinline__ TUTTI_LDS E *in_lds(uint32_t at) {
+  return reinterpret_cast<TUTTI_LDS E *>(static_cast<uintptr_t>(at));
+}
 
 template <typename T>
 __device__ __forceinline__ f32x16 wide_product(typename T::eight a, typename T::eight b, f32x16 c) {
@@ -726,82 +741,111 @@ __global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const A
     __syncthreads();
   }
 
-  // a tile's blocks, one key to a lane
   bool skipped = false;
+  struct Tile {
+    uint64_t oks;              // its keys that some row sees and that are there
+    float f[4], lg[4], rc[4];  // e4m3, PAGED16: of each 16 keys, the factor of the scores, log2 and reciprocal of the values' scale
+  };
+  Tile next{}, now{};
+  u32x4 raw[E4M3 ? DP / 32 : 1];
+  constexpr uint32_t CHUNKS = kWideTile * DP * EB / 4096;   // 1 KiB each, of a plane, that a wavefront brings: 16 rows
+  constexpr uint32_t LANES_A_ROW = DP * EB / 16, ROWS_A_CHUNK = kLanes / LANES_A_ROW;
+  static_assert(CHUNKS * ROWS_A_CHUNK == 16);
+  const uint32_t place = lane % LANES_A_ROW;
+  // chunk c of the wavefront's 16 rows: `at` + `in` in either plane
+  const auto bring = [&](uint32_t c, uint64_t at, uint32_t in, uint32_t row, uint32_t buffer) {
+    if constexpr (E4M3) {
+      raw[c] = raw[CHUNKS + c] = u32x4{0, 0, 0, 0};
+      if (place * 16 < d && (next.oks >> row & 1u)) {
+        raw[c] = *reinterpret_cast<const u32x4 *>(a.pool.k + at + (in + place * 16));
+        raw[CHUNKS + c] = *reinterpret_cast<const u32x4 *>(a.pool.v + at + (in + place * 16));
+      }
+    } else {
+      const uint32_t unit = place ^ swap_of<UNITS>(row);
+      if (unit * 8 < d) {
+        TUTTI_LDS uint8_t *to = base + buffer * BUFFER + (wave * CHUNKS + c) * 1024;
+        __builtin_amdgcn_global_load_lds((const TUTTI_GLOBAL void *)(a.pool.k + at + (in + unit * 16)), (TUTTI_LDS void *)to, 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((const TUTTI_GLOBAL void *)(a.pool.v + at + (in + unit * 16)), (TUTTI_LDS void *)(to + PLANE), 16, 0, 0);
+      }
+    }
+  };
+  const auto value_scale = [&](uint32_t id, bool ok, float &f, float &lg, float &rc) {
+    const float sv = a.pool.v_scale[id * a.pool.scale_stride + u.head];
+    // (f not 0: times 0, a score of -infinity would be no number)
+    f = ok ? fmaxf(factor * a.pool.k_scale[id * a.pool.scale_stride + u.head], 0x1p-120f) : 1.0f;
+    lg = ok ? __builtin_amdgcn_logf(sv) : 0.0f;
+    rc = ok ? __builtin_amdgcn_rcpf(sv) : 0.0f;
+  };
+  // PAGED16: 16 keys from a multiple of 16 on lie in one block.  Those of 16 tiles are looked up at once, 16 keys to a lane; a tile's
+  // come from there as uniform values, and the wavefront brings the 16 keys that are its own.
+  uint64_t off_l = 0;
+  Tile looked{};  // [0] of each: the lane's
+  const auto look_up_16 = [&](uint32_t tile0) {
+    const uint32_t key = tile0 * kWideTile + 16 * lane, n = block_of(a.pool, key);
+    const uint64_t at = static_cast<uint64_t>(s.table_off) + n;
+    bool ok = key < t1 * kWideTile && key + 16 > any_lo && key < any_hi;
+    uint32_t id = 0;
+    if (ok) {
+      if (at < a.batch.table_len) id = a.batch.table[at];
+      ok = at < a.batch.table_len && id < a.pool.num_blocks;
+      if (!ok) skipped = true;
+    }
+    if (!ok) id = 0;
+    off_l = id * a.pool.block_stride + head_at + static_cast<uint64_t>(key - n * a.pool.block_tokens) * ts;
+    if constexpr (E4M3) value_scale(id, ok, looked.f[0], looked.lg[0], looked.rc[0]);
+    looked.oks = __ballot(ok);
+  };
+  // else: one key to a lane, the next tile's ids on their way while this one's keys are brought
   uint32_t id_next = 0;
   bool ok_next = false;
-  const auto look_up = [&](uint32_t tile) {
+  const auto look_up_1 = [&](uint32_t tile) {
     const uint32_t key = tile * kWideTile + lane;
     const uint64_t at = static_cast<uint64_t>(s.table_off) + block_of(a.pool, key);
     ok_next = tile < t1 && key >= any_lo && key < any_hi;
     id_next = 0;
-    if (ok_next) {
-      if (at < a.batch.table_len)
-        id_next = a.batch.table[at];
-      else
-        id_next = ~0u;
-    }
+    if (ok_next) id_next = at < a.batch.table_len ? a.batch.table[at] : ~0u;
   };
-  struct Tile {
-    uint64_t oks;
-    float f[4], lg[4], rc[4];  // PAGED16: of each 16 keys
-  };
-  Tile next{}, now{};
-  u32x4 raw[E4M3 ? DP / 32 : 1];
-  constexpr uint32_t CHUNKS = kWideTile * DP * EB / 4096;   // 1 KiB each, of a plane, that a wavefront brings
-  constexpr uint32_t LANES_A_ROW = DP * EB / 16, ROWS_A_CHUNK = kLanes / LANES_A_ROW;
-  // asks for what look_up() has found
   const auto fetch = [&](uint32_t tile, uint32_t buffer) {
-    const uint32_t key = tile * kWideTile + lane;
-    if (ok_next && id_next >= a.pool.num_blocks) {
-      ok_next = false;
-      skipped = true;
-    }
-    const uint32_t id = ok_next ? id_next : 0, slot = key - block_of(a.pool, key) * a.pool.block_tokens;
-    const uint64_t off = id * a.pool.block_stride + head_at + static_cast<uint64_t>(slot) * ts;
-    next.oks = __ballot(ok_next);
-    if constexpr (E4M3) {
-      const float sv = a.pool.v_scale[id * a.pool.scale_stride + u.head];
-      // (not 0: times 0, a score of -infinity would be no number)
-      const float f = ok_next ? fmaxf(factor * a.pool.k_scale[id * a.pool.scale_stride + u.head], 0x1p-120f) : 1.0f;
-      const float lg = ok_next ? __builtin_amdgcn_logf(sv) : 0.0f, rc = ok_next ? 1.0f / sv : 0.0f;
-      if constexpr (PAGED16) {
-        // (a key that is not there may stand in front of one that is: the last of its 16 that is there speaks for all)
+    if constexpr (PAGED16) {
+      const uint32_t from = ((tile - t0) & 15u) * 4, key0 = tile * kWideTile;
+      if (from == 0) look_up_16(tile);
+      next.oks = 0;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const uint32_t some = static_cast<uint32_t>(next.oks >> (16 * x)) & 0xffffu;
-          const uint32_t from = 16 * x + (some ? 31 - __builtin_clz(some) : 0);
-          next.f[x] = __uint_as_float(from_lane(__float_as_uint(f), from));
-          next.lg[x] = __uint_as_float(from_lane(__float_as_uint(lg), from));
-          next.rc[x] = __uint_as_float(from_lane(__float_as_uint(rc), from));
+      for (int x = 0; x < 4; ++x) {
+        if (looked.oks >> (from + x) & 1u) next.oks |= 0xffffull << (16 * x);
+        if constexpr (E4M3) {
+          next.f[x] = __uint_as_float(from_lane(__float_as_uint(looked.f[0]), from + x));
+          next.lg[x] = __uint_as_float(from_lane(__float_as_uint(looked.lg[0]), from + x));
+          next.rc[x] = __uint_as_float(from_lane(__float_as_uint(looked.rc[0]), from + x));
         }
-      } else {
-        next.f[0] = f;   // per lane: to LDS when the tile's turn comes
-        next.lg[0] = lg;
-        next.rc[0] = rc;
       }
-    }
+      if (key0 < any_lo) next.oks &= ~0ull << (any_lo - key0);
+      if (key0 + kWideTile > any_hi) next.oks &= ~(~0ull << (any_hi - key0));  // (key0 < any_hi)
+      const uint64_t at = static_cast<uint64_t>(from_lane(static_cast<uint32_t>(off_l >> 32), from + wave)) << 32 |
+                          from_lane(static_cast<uint32_t>(off_l), from + wave);
 #pragma unroll
-    for (uint32_t c = 0; c < CHUNKS; ++c) {
-      const uint32_t row = (wave * CHUNKS + c) * ROWS_A_CHUNK + lane / LANES_A_ROW, place = lane % LANES_A_ROW;
-      const uint64_t from = static_cast<uint64_t>(__shfl(static_cast<uint32_t>(off >> 32), row, kLanes)) << 32 |
+      for (uint32_t c = 0; c < CHUNKS; ++c) {
+        const uint32_t in = c * ROWS_A_CHUNK + lane / LANES_A_ROW;
+        bring(c, at, in * ts, wave * 16 + in, buffer);
+      }
+    } else {
+      const uint32_t key = tile * kWideTile + lane;
+      if (ok_next && id_next >= a.pool.num_blocks) {
+        ok_next = false;
+        skipped = true;
+      }
+      const uint32_t id = ok_next ? id_next : 0, slot = key - block_of(a.pool, key) * a.pool.block_tokens;
+      const uint64_t off = id * a.pool.block_stride + head_at + static_cast<uint64_t>(slot) * ts;
+      next.oks = __ballot(ok_next);
+      if constexpr (E4M3) value_scale(id, ok_next, next.f[0], next.lg[0], next.rc[0]);  // per lane: to LDS when the tile's turn comes
+#pragma unroll
+      for (uint32_t c = 0; c < CHUNKS; ++c) {
+        const uint32_t row = (wave * CHUNKS + c) * ROWS_A_CHUNK + lane / LANES_A_ROW;
+        const uint64_t at = static_cast<uint64_t>(__shfl(static_cast<uint32_t>(off >> 32), row, kLanes)) << 32 |
                             __shfl(static_cast<uint32_t>(off), row, kLanes);
-      if constexpr (E4M3) {
-        const bool in = place * 16 < d;
-        const bool ok = next.oks >> row & 1u;
-        raw[c] = raw[CHUNKS + c] = u32x4{0, 0, 0, 0};
-        if (in && ok) {
-          raw[c] = *reinterpret_cast<const u32x4 *>(a.pool.k + from + place * 16);
-          raw[CHUNKS + c] = *reinterpret_cast<const u32x4 *>(a.pool.v + from + place * 16);
-        }
-      } else {
-        const uint32_t unit = place ^ (row & (UNITS - 1));
-        if (unit * 8 < d) {
-          TUTTI_LDS uint8_t *to = base + buffer * BUFFER + (wave * CHUNKS + c) * 1024;
-          __builtin_amdgcn_global_load_lds((const TUTTI_GLOBAL void *)(a.pool.k + from + unit * 16), (TUTTI_LDS void *)to, 16, 0, 0);
-          __builtin_amdgcn_global_load_lds((const TUTTI_GLOBAL void *)(a.pool.v + from + unit * 16), (TUTTI_LDS void *)(to + PLANE), 16, 0, 0);
-        }
+        bring(c, at, 0, row, buffer);
       }
+      look_up_1(tile + 1);
     }
   };
   // e4m3: widens what fetch() has brought
@@ -810,12 +854,12 @@ __global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const A
 #pragma unroll
       for (uint32_t c = 0; c < 2 * CHUNKS; ++c) {
         const bool value = c >= CHUNKS;
-        const uint32_t row = (wave * CHUNKS + c % CHUNKS) * ROWS_A_CHUNK + lane / LANES_A_ROW, place = lane % LANES_A_ROW;
+        const uint32_t row = (wave * CHUNKS + c % CHUNKS) * ROWS_A_CHUNK + lane / LANES_A_ROW;
         TUTTI_LDS uint8_t *to = base + buffer * BUFFER + (value ? PLANE : 0) + row * ROW_BYTES;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           const u32x2 codes = {raw[c][2 * x], raw[c][2 * x + 1]};
-          const uint32_t unit = (2 * place + x) ^ (row & (UNITS - 1));
+          const uint32_t unit = (2 * place + x) ^ swap_of<UNITS>(row);
           u32x4 w;
           if (value)
             w = __builtin_bit_cast(u32x4, widen<Fp16>(codes));
@@ -827,31 +871,35 @@ __global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const A
     }
   };
 
-  // where a lane reads: keys, per step of 16 values; values, per exclusive-or of their unit
-  uint32_t key_at[STEPS], value_at[4];
+  // where a lane reads: its key's row, from which step j is 2j units away by exclusive or; its four values' rows of 8, from which 32
+  // values further on are 4 units away
+  const uint32_t key_at = r * ROW_BYTES + (hf ^ swap_of<UNITS>(r)) * 16;
+  uint32_t value_at[2];
 #pragma unroll
-  for (int j = 0; j < STEPS; ++j) key_at[j] = r * ROW_BYTES + ((2 * j + hf) ^ (r & (UNITS - 1))) * 16;
-  {
-    const uint32_t j = lane & 15u, grp = lane >> 4, row = 4 * (grp >> 1) + j / 4;
-    const uint32_t unit = (2 * (grp & 1u) + (j & 3u) / 2) ^ row;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) value_at[x] = PLANE + row * ROW_BYTES + (unit ^ (x << 2)) * 16 + (j & 1u) * 8;
+  for (int c = 0; c < 2; ++c) {
+    const uint32_t j = lane & 15u, row = 8 * c + 4 * hf + j / 4, unit = 2 * (lane >> 4 & 1u) + (j & 3u) / 2;
+    value_at[c] = PLANE + row * ROW_BYTES + (unit ^ swap_of<UNITS>(row)) * 16 + (j & 1u) * 8;
   }
-
   // keys 16x.. of the tile, values 32n..: what the products take
-  const auto values_of = [&](TUTTI_LDS uint8_t *from, int n, int x) {
+  const auto values_of = [&](uint32_t from, int n, int x) {
     s16x4 v[2];
 #pragma unroll
     for (int c = 0; c < 2; ++c)
-      v[c] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (TUTTI_LDS s16x4 *)(from + value_at[DP == 128 ? n ^ (2 * c) : n] + (16 * x + 8 * c) * ROW_BYTES));
+      v[c] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(in_lds<s16x4>(((from + value_at[c]) ^ (n << 6)) + 16 * x * ROW_BYTES));
     return __builtin_bit_cast(typename P::eight, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  // which keys of a tile a lane's row sees: bit c for key c + 4*hf of it
+  const auto seen_of = [&](int t, uint32_t key0) {
+    const uint32_t from = lo[t] > key0 ? min(lo[t] - key0, kWideTile) : 0, to = hi[t] > key0 ? min(hi[t] - key0, kWideTile) : 0;
+    uint64_t bits = now.oks;
+    bits &= from < 64 ? ~0ull << from : 0;
+    bits &= to < 64 ? ~(~0ull << to) : ~0ull;
+    return bits >> (4 * hf);
   };
 
   if (t1 > t0) {
-    look_up(t0);
+    if (!PAGED16) look_up_1(t0);
     fetch(t0, 0);
-    look_up(t0 + 1);
     put(0);
   }
   for (uint32_t tile = t0; tile < t1; ++tile) {
@@ -865,11 +913,9 @@ __global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const A
       per_key[wave][1][lane] = now.lg[0];
       per_key[wave][2][lane] = now.rc[0];
     }
-    if (more) {
-      fetch(tile + 1, buffer ^ 1u);
-      look_up(tile + 2);
-    }
+    if (more) fetch(tile + 1, buffer ^ 1u);
     TUTTI_LDS uint8_t *const here = base + buffer * BUFFER;
+    const uint32_t here_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(here));
     const bool wg_edge = key0 < all_lo || key0 + kWideTile > all_hi || now.oks != ~0ull;
     bool odd = false;
     if (wg_edge) {
@@ -897,19 +943,38 @@ __global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const A
       const bool edge = key0 < w_all_lo || key0 + kWideTile > w_all_hi || now.oks != ~0ull;
       typename P::eight p[RW][4];
       f32x16 sc[RW][2];
+      {
+        // the reads of half the keys are under way before the first product, those of the others while it goes on
+        u32x4 k[2][STEPS];
+        const auto read = [&](int h, int from, int to) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+          for (int j = from; j < to; ++j) k[h][j] = *in_lds<u32x4>(((here_at + key_at) ^ (j << 5)) + h * 32 * ROW_BYTES);
+          __builtin_amdgcn_sched_barrier(0);
+        };
+        const auto multiply = [&](int h, int from, int to) {
 #pragma unroll
-        for (int t = 0; t < RW; ++t)
+          for (int j = from; j < to; ++j)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) sc[t][h][i] = 0.0f;
+            for (int t = 0; t < RW; ++t) sc[t][h] = wide_product<T>(__builtin_bit_cast(typename T::eight, k[h][j]), q[t][j], sc[t][h]);
+          __builtin_amdgcn_sched_barrier(0);
+        };
+        read(0, 0, STEPS);
 #pragma unroll
-        for (int j = 0; j < STEPS; ++j) {
-          const typename T::eight k = __builtin_bit_cast(typename T::eight, *(TUTTI_LDS u32x4 *)(here + key_at[j] + h * 32 * ROW_BYTES));
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int t = 0; t < RW; ++t) sc[t][h] = wide_product<T>(k, q[t][j], sc[t][h]);
-        }
+          for (int t = 0; t < RW; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[t][h][i] = 0.0f;
+        read(1, 0, STEPS / 2);
+        multiply(0, 0, STEPS / 2);
+        read(1, STEPS / 2, STEPS);
+        multiply(0, STEPS / 2, STEPS);
+        multiply(1, 0, STEPS);
       }
+      typename P::eight v[2][DT];  // of the 16 keys whose turn it is, and of the next
+#pragma unroll
+      for (int n = 0; n < DT; ++n) v[0][n] = values_of(here_at, n, 0);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int t = 0; t < RW; ++t) {
         if (E4M3 && !PAGED16) {
@@ -924,13 +989,13 @@ __global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const A
             }
         }
         if (edge) {
+          asm volatile("" ::);  // (a branch: most tiles are whole ones)
+          const uint64_t seen = seen_of(t, key0);
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const uint32_t in = 32 * h + 8 * (i / 4) + 4 * hf + i % 4, key = key0 + in;
-              if (!(now.oks >> in & 1u) || key < lo[t] || key >= hi[t]) sc[t][h][i] = -__builtin_inff();
-            }
+            for (int i = 0; i < 16; ++i)
+              if (!(seen >> (32 * h + 8 * (i / 4) + i % 4) & 1u)) sc[t][h][i] = -__builtin_inff();
         }
         // the largest of each 16 keys, then with their factors of all
         float top = kLowest;
@@ -969,13 +1034,16 @@ __global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const A
         }
       }
 #pragma unroll
-      for (int x = 0; x < 4; ++x)
+      for (int x = 0; x < 4; ++x) {
+        if (x < 3)
 #pragma unroll
-        for (int n = 0; n < DT; ++n) {
-          const typename P::eight both = values_of(here, n, x);
+          for (int n = 0; n < DT; ++n) v[(x + 1) & 1][n] = values_of(here_at, n, x + 1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int t = 0; t < RW; ++t) o[t][n] = wide_product<P>(both, p[t][x], o[t][n]);
-        }
+        for (int n = 0; n < DT; ++n)
+#pragma unroll
+          for (int t = 0; t < RW; ++t) o[t][n] = wide_product<P>(v[x & 1][n], p[t][x], o[t][n]);
+      }
     }
     if (odd) {
       // the infinities and NaN of the tile as numbers that say what they are, for the rows that see them: 1, 2^7 and 2^14, sums of
@@ -983,7 +1051,7 @@ __global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const A
       __syncthreads();
 #pragma unroll 1
       for (uint32_t x = threadIdx.x; x < PLANE / 16; x += 256) {
-        const uint32_t row = x / UNITS, d0 = ((x % UNITS) ^ (row & (UNITS - 1))) * 8, key = key0 + row;
+        const uint32_t row = x / UNITS, d0 = ((x % UNITS) ^ swap_of<UNITS>(row)) * 8, key = key0 + row;
         typename P::eight w = {};
         if (d0 < d && key >= any_lo && key < any_hi) {
           const uint32_t n = block_of(a.pool, key);
@@ -1011,15 +1079,13 @@ __global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const A
             for (int i = 0; i < 16; ++i) sums[t][i] = 0.0f;
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            const typename P::eight v = values_of(here, n, x);
+            const typename P::eight v = values_of(here_at, n, x);
 #pragma unroll
             for (int t = 0; t < RW; ++t) {
+              const uint64_t bits = seen_of(t, key0);
               typename P::eight seen;
 #pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const uint32_t key = key0 + 16 * x + 8 * (i / 4) + 4 * hf + i % 4;
-                seen[i] = static_cast<typename P::one>(key >= lo[t] && key < hi[t] ? 1.0f : 0.0f);
-              }
+              for (int i = 0; i < 8; ++i) seen[i] = static_cast<typename P::one>(bits >> (16 * x + 8 * (i / 4) + i % 4) & 1u ? 1.0f : 0.0f);
               sums[t] = wide_product<P>(v, seen, sums[t]);
             }
           }
