@@ -111,11 +111,11 @@ __device__ __forceinline__ Unit locate(const AttendArgs &a, const Plan &p, uint3
       u.seq = base + l;
       u.s = tutti_seq{from_lane(s.row0, l), from_lane(s.n_new, l), from_lane(s.n_held, l), from_lane(s.table_off, l)};
       u.parts = from_lane(parts, l);
-      // heads first, then parts, then row tiles: neighbours read the same blocks
+      // heads first, then parts, then row tiles, the last ones, which see most keys, in front: neighbours read the same blocks
       const uint32_t head_groups = a.kv_heads / a.abreast;
       u.head = local % head_groups * a.abreast;
       u.part = local / head_groups % u.parts;
-      u.row_tile = local / head_groups / u.parts;
+      u.row_tile = from_lane(tiles, l) - 1 - local / head_groups / u.parts;
       u.part_slot = from_lane(split_upto, l) - from_lane(split, l) + (u.row_tile * a.kv_heads + u.head) * u.parts;
       if (!first) return u;
     }
@@ -966,10 +966,12 @@ __global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const A
 #pragma unroll
             for (int i = 0; i < 16; ++i) sc[t][h][i] = 0.0f;
         read(1, 0, STEPS / 2);
+        __builtin_amdgcn_s_setprio(1);  // the other wavefront's arithmetic fits between matrix instructions, not the other way round
         multiply(0, 0, STEPS / 2);
         read(1, STEPS / 2, STEPS);
         multiply(0, STEPS / 2, STEPS);
         multiply(1, 0, STEPS);
+        __builtin_amdgcn_s_setprio(0);
       }
       typename P::eight v[2][DT];  // of the 16 keys whose turn it is, and of the next
 #pragma unroll
@@ -1039,12 +1041,14 @@ __global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const A
 #pragma unroll
           for (int n = 0; n < DT; ++n) v[(x + 1) & 1][n] = values_of(here_at, n, x + 1);
         __builtin_amdgcn_sched_barrier(0);
+        if (x == 0) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int n = 0; n < DT; ++n)
 #pragma unroll
           for (int t = 0; t < RW; ++t) o[t][n] = wide_product<P>(v[x & 1][n], p[t][x], o[t][n]);
       }
     }
+    __builtin_amdgcn_s_setprio(0);
     if (odd) {
       // the infinities and NaN of the tile as numbers that say what they are, for the rows that see them: 1, 2^7 and 2^14, sums of
       // 64 of which say which there were
@@ -1165,10 +1169,10 @@ template <typename T, int DP, int ROWS, int WAVES>
 __global__ __launch_bounds__(256) void k_kv_join(const AttendArgs a) {
   constexpr uint32_t TP = DP / 4, ABREAST = WAVES * kLanes / TP, U = 4;
   const uint32_t lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
-  const uint32_t item = WAVES == 4 ? blockIdx.x : blockIdx.x * 4 + uniform(wave);
   const uint32_t thread = WAVES == 4 ? threadIdx.x : lane;   // among those of the row
   const Plan plan = make_plan<ROWS>(a);
   // items: rows of the sequences that are split
+  for (uint32_t item = WAVES == 4 ? blockIdx.x : blockIdx.x * 4 + uniform(wave);; item += gridDim.x * (4 / WAVES)) {
   uint32_t before = 0, slots = 0, units = 0;
   bool found = false;
   uint32_t row0 = 0, parts = 0, local = 0, first_slot = 0, units_upto_it = 0;
@@ -1207,7 +1211,7 @@ __global__ __launch_bounds__(256) void k_kv_join(const AttendArgs a) {
   const uint32_t kv = head / a.group, row = i * a.group + head - kv * a.group;
   const uint32_t slot = first_slot + (row / ROWS * a.kv_heads + kv) * parts;
   // what the attention kernel did not do is not joined
-  if (slot + parts > a.max_parts || units_upto_it > a.max_units) return;
+  if (slot + parts > a.max_parts || units_upto_it > a.max_units) continue;
   const uint64_t at0 = static_cast<uint64_t>(slot) * ROWS + row % ROWS;
 
   float top = kLowest;
@@ -1255,7 +1259,7 @@ __global__ __launch_bounds__(256) void k_kv_join(const AttendArgs a) {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
-  if (thread * 2 >= a.d) return;
+  if (thread * 2 < a.d) {
   float total = 0.0f;
   f32x2 z = {0, 0};
 #pragma unroll
@@ -1270,6 +1274,14 @@ __global__ __launch_bounds__(256) void k_kv_join(const AttendArgs a) {
   if (thread == 0 && a.lse)
     a.lse[static_cast<uint64_t>(row0 + i) * heads + head] =
         total == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(total)) * kLn2;
+  }
+  if constexpr (WAVES == 4) {
+    __syncthreads();  // LDS is the next row's
+  } else {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+  }
 }
 
 }  // namespace tutti
