@@ -185,17 +185,17 @@ template <typename T, bool E4M3, bool PAGED16>
 void launch_wide(const AttendArgs &a, hipStream_t stream) {
   const dim3 grid(a.max_units), wg(256);
   if (a.d == 128)
-    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 128, true, PAGED16, 1>), grid, wg, 0, stream, a);
+    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 128, true, PAGED16>), grid, wg, 0, stream, a);
   else if (a.d == 112)
-    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 112, true, PAGED16, 1>), grid, wg, 0, stream, a);
+    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 112, true, PAGED16>), grid, wg, 0, stream, a);
   else if (a.d == 96)
-    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 96, true, PAGED16, 1>), grid, wg, 0, stream, a);
+    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 96, true, PAGED16>), grid, wg, 0, stream, a);
   else if (a.d == 80)
-    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 80, true, PAGED16, 1>), grid, wg, 0, stream, a);
+    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 80, true, PAGED16>), grid, wg, 0, stream, a);
   else if (a.d == 64)
-    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 64, true, PAGED16, 1>), grid, wg, 0, stream, a);
+    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 64, true, PAGED16>), grid, wg, 0, stream, a);
   else
-    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 64, false, PAGED16, 1>), grid, wg, 0, stream, a);
+    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 64, false, PAGED16>), grid, wg, 0, stream, a);
 }
 template <typename T, bool E4M3, int DP>
 void launch_attend(const AttendArgs &a, uint32_t rows, hipStream_t stream) {

@@ -613,7 +613,7 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 ? 3 : 2) void k_kv_attend(
   }
 }
 
-// ---- Many queries: a workgroup of four wavefronts takes 128*RW rows of queries, a KV head and a part of the keys, 64 at a time.
+// ---- Many queries: a workgroup of four wavefronts takes 128 rows of queries, a KV head and a part of the keys, 64 at a time.
 //
 // A tile of keys and values lies in LDS as 16-bit rows, twice: while one is worked on the next is on its way (16-bit blocks straight
 // from memory to LDS, e4m3 through registers, where it is widened).  Units of 16 bytes are swapped within a row by the row's number, so
@@ -661,14 +661,15 @@ __device__ __forceinline__ float sum_of_halves(float x) {
 }
 
 // D: values of a head that it is built for; FULL: a head has so many (else fewer than 64, and D is 64).
-template <typename T, bool E4M3, int D, bool FULL, bool PAGED16, int RW>
-__global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const AttendArgs a) {
-  constexpr int DP = D <= 64 ? 64 : 128, ROWS = 128 * RW, STEPS = D / 16, DT = (D + 31) / 32;
-  constexpr uint32_t UNITS = DP / 8, ROW_BYTES = DP * 2, PLANE = kWideTile * ROW_BYTES, BUFFER = 2 * PLANE;
+template <typename T, bool E4M3, int D, bool FULL, bool PAGED16>
+__global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
+  constexpr int DP = D <= 64 ? 64 : 128, ROWS = 128, STEPS = D / 16, DT = (D + 31) / 32;
+  constexpr uint32_t UNITS = DP / 8, ROW_BYTES = DP * 2, PLANE = kWideTile * ROW_BYTES;
   constexpr uint32_t EB = E4M3 ? 1 : 2;
   using P = std::conditional_t<E4M3, Fp16, T>;
   const uint32_t d = FULL ? D : a.d;
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * BUFFER];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * PLANE];
+  __shared__ uint32_t not_finite[4];  // a wavefront has met an infinity or NaN among the values of a tile that has an edge
   __shared__ float per_key[E4M3 && !PAGED16 ? 4 : 1][3][kWideTile];
 
   const uint32_t lane = threadIdx.x & (kLanes - 1), wave = uniform(threadIdx.x / kLanes);
@@ -692,7 +693,7 @@ __global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const A
   const uint32_t row_a = u.row_tile * ROWS, row_b = min(row_a + ROWS, n_rows) - 1;
   const uint32_t place_a = begin + row_a / a.group, place_b = begin + row_b / a.group;
   const uint32_t any_lo = uniform(low(place_a)), any_hi = uniform(high(place_b)), all_lo = uniform(low(place_b)), all_hi = uniform(high(place_a));
-  const uint32_t wave_a = row_a + wave * 32 * RW, wave_b = min(wave_a + 32 * RW, n_rows);
+  const uint32_t wave_a = row_a + wave * 32, wave_b = min(wave_a + 32, n_rows);
   const bool has_rows = wave_a < wave_b;
   const uint32_t w_place_a = has_rows ? begin + wave_a / a.group : 0, w_place_b = has_rows ? begin + (wave_b - 1) / a.group : 0;
   const uint32_t w_any_lo = uniform(low(w_place_a)), w_any_hi = has_rows ? uniform(high(w_place_b)) : 0;
@@ -701,101 +702,140 @@ __global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const A
   const uint32_t t0 = uniform(tile_lo + static_cast<uint32_t>(static_cast<uint64_t>(tiles) * u.part / u.parts));
   const uint32_t t1 = uniform(tile_lo + static_cast<uint32_t>(static_cast<uint64_t>(tiles) * (u.part + 1) / u.parts));
 
-  uint32_t lo[RW], hi[RW];
-  typename T::eight q[RW][STEPS];
+  uint32_t lo, hi;  // of the lane's row
+  typename T::eight q[STEPS];
   const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0;  // scores are multiplied by a factor that is positive
   const float factor = fmaxf(fabsf(a.scale_log2), 0x1p-100f);   // (0: no score counts; times 0, a masked one would be no number)
-#pragma unroll
-  for (int t = 0; t < RW; ++t) {
-    const uint32_t row = wave_a + t * 32 + r;
+  {
+    const uint32_t row = wave_a + r;
     const bool in = row < n_rows;
     const uint32_t i = in ? row / a.group : 0, head = u.head * a.group + (in ? row - i * a.group : 0);
-    hi[t] = high(begin + i);
-    lo[t] = low(begin + i);
+    hi = high(begin + i);
+    lo = low(begin + i);
     const uint8_t *at = static_cast<const uint8_t *>(a.q.base) + static_cast<uint64_t>(s.row0 + i) * a.q.row_stride + head * a.q.head_stride;
 #pragma unroll
     for (int j = 0; j < STEPS; ++j) {
-      u32x4 w = {0, 0, 0, 0};
-      if (FULL || j * 16 < static_cast<int>(d)) w = *reinterpret_cast<const u32x4 *>(at + j * 32 + hf * 16);
-      w ^= u32x4{flip, flip, flip, flip};
-      q[t][j] = __builtin_bit_cast(typename T::eight, w);
+      u32x4 x = {0, 0, 0, 0};
+      if (FULL || j * 16 < static_cast<int>(d)) x = *reinterpret_cast<const u32x4 *>(at + j * 32 + hf * 16);
+      x ^= u32x4{flip, flip, flip, flip};
+      q[j] = __builtin_bit_cast(typename T::eight, x);
     }
   }
-  f32x16 o[RW][DT];
-  float m[RW], l[RW];
+  f32x16 o[DT];
+  float m = kLowest, l = 0.0f;
 #pragma unroll
-  for (int t = 0; t < RW; ++t) {
-    m[t] = kLowest;
-    l[t] = 0.0f;
+  for (int n = 0; n < DT; ++n)
 #pragma unroll
-    for (int n = 0; n < DT; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[t][n][i] = 0.0f;
-  }
+    for (int i = 0; i < 16; ++i) o[n][i] = 0.0f;
 
   const uint64_t head_at = static_cast<uint64_t>(u.head) * a.pool.head_stride;
   const uint32_t ts = a.pool.token_stride;
   TUTTI_LDS uint8_t *const base = (TUTTI_LDS uint8_t *)lds;
+  const uint32_t lds_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(base));
+  if (threadIdx.x < 4) not_finite[threadIdx.x] = 0;
   if (!FULL || D != DP) {  // units behind the rows' ends are never written: what lies there meets weights
-    for (uint32_t x = threadIdx.x * 16; x < 2 * BUFFER; x += 256 * 16) *(TUTTI_LDS u32x4 *)(base + x) = u32x4{0, 0, 0, 0};
+    for (uint32_t x = threadIdx.x * 16; x < 4 * PLANE; x += 256 * 16) *(TUTTI_LDS u32x4 *)(base + x) = u32x4{0, 0, 0, 0};
     __syncthreads();
   }
 
   bool skipped = false;
   struct Tile {
-    uint64_t oks;              // its keys that some row sees and that are there
-    float f[4], lg[4], rc[4];  // e4m3, PAGED16: of each 16 keys, the factor of the scores, log2 and reciprocal of the values' scale
+    uint64_t oks;      // its keys that some row sees and that are there
+    uint64_t at;       // !PAGED16: where the lane's key is, from a plane's begin; e4m3: its factor of the scores, log2 and reciprocal of
+    float f, lg, rc;   // the values' scale
   };
-  Tile next{}, now{};
-  u32x4 raw[E4M3 ? DP / 32 : 1];
+  Tile now{}, next{}, second{};  // the tile in work, the next (its values are on their way), the one after that (its keys)
+  u32x4 raw_k[E4M3 ? DP / 64 : 1], raw_v[E4M3 ? DP / 64 : 1];
   constexpr uint32_t CHUNKS = kWideTile * DP * EB / 4096;   // 1 KiB each, of a plane, that a wavefront brings: 16 rows
   constexpr uint32_t LANES_A_ROW = DP * EB / 16, ROWS_A_CHUNK = kLanes / LANES_A_ROW;
   static_assert(CHUNKS * ROWS_A_CHUNK == 16);
-  const uint32_t place = lane % LANES_A_ROW;
-  // chunk c of the wavefront's 16 rows: `at` + `in` in either plane
-  const auto bring = [&](uint32_t c, uint64_t at, uint32_t in, uint32_t row, uint32_t buffer) {
-    if constexpr (E4M3) {
-      raw[c] = raw[CHUNKS + c] = u32x4{0, 0, 0, 0};
-      if (place * 16 < d && (next.oks >> row & 1u)) {
-        raw[c] = *reinterpret_cast<const u32x4 *>(a.pool.k + at + (in + place * 16));
-        raw[CHUNKS + c] = *reinterpret_cast<const u32x4 *>(a.pool.v + at + (in + place * 16));
-      }
-    } else {
-      const uint32_t unit = place ^ swap_of<UNITS>(row);
-      if (unit * 8 < d) {
-        TUTTI_LDS uint8_t *to = base + buffer * BUFFER + (wave * CHUNKS + c) * 1024;
-        __builtin_amdgcn_global_load_lds((const TUTTI_GLOBAL void *)(a.pool.k + at + (in + unit * 16)), (TUTTI_LDS void *)to, 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((const TUTTI_GLOBAL void *)(a.pool.v + at + (in + unit * 16)), (TUTTI_LDS void *)(to + PLANE), 16, 0, 0);
-      }
-    }
-  };
-  const auto value_scale = [&](uint32_t id, bool ok, float &f, float &lg, float &rc) {
+  const auto scale_of = [&](uint32_t id, bool ok, float &f, float &lg, float &rc) {
     const float sv = a.pool.v_scale[id * a.pool.scale_stride + u.head];
     // (f not 0: times 0, a score of -infinity would be no number)
     f = ok ? fmaxf(factor * a.pool.k_scale[id * a.pool.scale_stride + u.head], 0x1p-120f) : 1.0f;
     lg = ok ? __builtin_amdgcn_logf(sv) : 0.0f;
     rc = ok ? __builtin_amdgcn_rcpf(sv) : 0.0f;
   };
-  // PAGED16: 16 keys from a multiple of 16 on lie in one block.  Those of 16 tiles are looked up at once, 16 keys to a lane; a tile's
-  // come from there as uniform values, and the wavefront brings the 16 keys that are its own.
-  uint64_t off_l = 0;
-  Tile looked{};  // [0] of each: the lane's
+  // PAGED16: 16 keys from a multiple of 16 on lie in one block.  Those of 16 tiles are looked up at once, 16 keys to a lane, and from
+  // the tile in work on again when the one after the next is none of them; a tile's come from there as uniform values, and the
+  // wavefront brings the 16 keys that are its own.
+  struct {
+    uint32_t tile;     // the first
+    uint64_t oks, at;  // which lanes' keys are there; where the lane's are, from a plane's begin
+    float f, lg, rc;
+  } looked{};
   const auto look_up_16 = [&](uint32_t tile0) {
+    looked.tile = tile0;
     const uint32_t key = tile0 * kWideTile + 16 * lane, n = block_of(a.pool, key);
     const uint64_t at = static_cast<uint64_t>(s.table_off) + n;
     bool ok = key < t1 * kWideTile && key + 16 > any_lo && key < any_hi;
     uint32_t id = 0;
+    const bool asked = ok;
     if (ok) {
       if (at < a.batch.table_len) id = a.batch.table[at];
       ok = at < a.batch.table_len && id < a.pool.num_blocks;
-      if (!ok) skipped = true;
     }
+    skipped |= __ballot(asked && !ok) != 0;
     if (!ok) id = 0;
-    off_l = id * a.pool.block_stride + head_at + static_cast<uint64_t>(key - n * a.pool.block_tokens) * ts;
-    if constexpr (E4M3) value_scale(id, ok, looked.f[0], looked.lg[0], looked.rc[0]);
+    looked.at = id * a.pool.block_stride + head_at + static_cast<uint64_t>(key - n * a.pool.block_tokens) * ts;
+    if constexpr (E4M3) scale_of(id, ok, looked.f, looked.lg, looked.rc);
     looked.oks = __ballot(ok);
   };
-  // else: one key to a lane, the next tile's ids on their way while this one's keys are brought
+  // brings the wavefront's 16 rows of a tile from a plane
+  const auto bring = [&](const uint8_t *plane, uint32_t tile, const Tile &t, uint32_t to_at, u32x4 (&raw)[E4M3 ? DP / 64 : 1]) {
+    // PAGED16: an address for all lanes, in scalar registers, and what a lane adds to it
+    uintptr_t rows = reinterpret_cast<uintptr_t>(plane);
+    if constexpr (PAGED16) {
+      const uint32_t from = (tile - looked.tile) * 4 + wave;
+      rows += static_cast<uint64_t>(from_lane(static_cast<uint32_t>(looked.at >> 32), from)) << 32 | from_lane(static_cast<uint32_t>(looked.at), from);
+      asm volatile("" : "+s"(rows));
+    }
+    const uint32_t oks = static_cast<uint32_t>(t.oks >> (wave * 16));
+    uint32_t l = lane;
+    if constexpr (E4M3) asm volatile("" : "+v"(l));  // (what follows from it is worked out anew: it has no registers to wait in)
+    const uint32_t place = l % LANES_A_ROW;
+#pragma unroll
+    for (uint32_t c = 0; c < CHUNKS; ++c) {
+      const uint32_t in = c * ROWS_A_CHUNK + l / LANES_A_ROW, row = wave * 16 + in;
+      if constexpr (!PAGED16)
+        rows = reinterpret_cast<uintptr_t>(plane) + (static_cast<uint64_t>(__shfl(static_cast<uint32_t>(t.at >> 32), row, kLanes)) << 32 |
+                                                     __shfl(static_cast<uint32_t>(t.at), row, kLanes));
+      const TUTTI_GLOBAL uint8_t *from = reinterpret_cast<const TUTTI_GLOBAL uint8_t *>(rows);
+      const uint32_t unit = E4M3 ? place : place ^ swap_of<UNITS>(row);
+      uint32_t off = (PAGED16 ? in * ts : 0) + unit * 16;
+      const bool inside = unit * 16 < d * EB;
+      if constexpr (E4M3) {
+        raw[c] = u32x4{0, 0, 0, 0};
+        if (inside && (oks >> in & 1u)) {
+          asm volatile("" : "+v"(off));  // (32 bits, to be added to the scalar address by the load)
+          raw[c] = *reinterpret_cast<const TUTTI_GLOBAL u32x4 *>(from + off);
+        }
+      } else if (inside) {
+        asm volatile("" : "+v"(off));
+        __builtin_amdgcn_global_load_lds((const TUTTI_GLOBAL void *)(from + off),
+                                         (TUTTI_LDS void *)(base + to_at + (wave * CHUNKS + c) * 1024), 16, 0, 0);
+      }
+    }
+  };
+  // e4m3: widens what bring() has brought
+  const auto put = [&](uint32_t to_at, const u32x4 (&raw)[E4M3 ? DP / 64 : 1], auto to_type) {
+    if constexpr (E4M3) {
+      uint32_t l = lane;
+      asm volatile("" : "+v"(l));
+      const uint32_t place = l % LANES_A_ROW;
+#pragma unroll
+      for (uint32_t c = 0; c < CHUNKS; ++c) {
+        const uint32_t row = wave * 16 + c * ROWS_A_CHUNK + l / LANES_A_ROW;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const uint32_t unit = (2 * place + x) ^ swap_of<UNITS>(row);
+          *(TUTTI_LDS u32x4 *)(base + to_at + row * ROW_BYTES + unit * 16) =
+              __builtin_bit_cast(u32x4, widen<decltype(to_type)>(u32x2{raw[c][2 * x], raw[c][2 * x + 1]}));
+        }
+      }
+    }
+  };
+  // else: one key to a lane, the following tile's ids on their way while this one's keys are brought
   uint32_t id_next = 0;
   bool ok_next = false;
   const auto look_up_1 = [&](uint32_t tile) {
@@ -805,69 +845,27 @@ __global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const A
     id_next = 0;
     if (ok_next) id_next = at < a.batch.table_len ? a.batch.table[at] : ~0u;
   };
-  const auto fetch = [&](uint32_t tile, uint32_t buffer) {
+  const auto find = [&](uint32_t tile, Tile &t) {
     if constexpr (PAGED16) {
-      const uint32_t from = ((tile - t0) & 15u) * 4, key0 = tile * kWideTile;
-      if (from == 0) look_up_16(tile);
-      next.oks = 0;
+      const uint32_t key0 = tile * kWideTile;
+      if (tile - looked.tile >= 16) look_up_16(tile - 2);
+      const uint32_t four = static_cast<uint32_t>(looked.oks >> ((tile - looked.tile) * 4));
+      t.oks = 0;
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        if (looked.oks >> (from + x) & 1u) next.oks |= 0xffffull << (16 * x);
-        if constexpr (E4M3) {
-          next.f[x] = __uint_as_float(from_lane(__float_as_uint(looked.f[0]), from + x));
-          next.lg[x] = __uint_as_float(from_lane(__float_as_uint(looked.lg[0]), from + x));
-          next.rc[x] = __uint_as_float(from_lane(__float_as_uint(looked.rc[0]), from + x));
-        }
-      }
-      if (key0 < any_lo) next.oks &= ~0ull << (any_lo - key0);
-      if (key0 + kWideTile > any_hi) next.oks &= ~(~0ull << (any_hi - key0));  // (key0 < any_hi)
-      const uint64_t at = static_cast<uint64_t>(from_lane(static_cast<uint32_t>(off_l >> 32), from + wave)) << 32 |
-                          from_lane(static_cast<uint32_t>(off_l), from + wave);
-#pragma unroll
-      for (uint32_t c = 0; c < CHUNKS; ++c) {
-        const uint32_t in = c * ROWS_A_CHUNK + lane / LANES_A_ROW;
-        bring(c, at, in * ts, wave * 16 + in, buffer);
-      }
+      for (int x = 0; x < 4; ++x)
+        if (four >> x & 1u) t.oks |= 0xffffull << (16 * x);
+      if (key0 < any_lo) t.oks &= ~0ull << (any_lo - key0);
+      if (key0 + kWideTile > any_hi) t.oks &= ~(~0ull << (any_hi - key0));  // (key0 < any_hi)
     } else {
       const uint32_t key = tile * kWideTile + lane;
-      if (ok_next && id_next >= a.pool.num_blocks) {
-        ok_next = false;
-        skipped = true;
-      }
+      const bool lost = ok_next && id_next >= a.pool.num_blocks;
+      skipped |= __ballot(lost) != 0;
+      ok_next = ok_next && !lost;
       const uint32_t id = ok_next ? id_next : 0, slot = key - block_of(a.pool, key) * a.pool.block_tokens;
-      const uint64_t off = id * a.pool.block_stride + head_at + static_cast<uint64_t>(slot) * ts;
-      next.oks = __ballot(ok_next);
-      if constexpr (E4M3) value_scale(id, ok_next, next.f[0], next.lg[0], next.rc[0]);  // per lane: to LDS when the tile's turn comes
-#pragma unroll
-      for (uint32_t c = 0; c < CHUNKS; ++c) {
-        const uint32_t row = (wave * CHUNKS + c) * ROWS_A_CHUNK + lane / LANES_A_ROW;
-        const uint64_t at = static_cast<uint64_t>(__shfl(static_cast<uint32_t>(off >> 32), row, kLanes)) << 32 |
-                            __shfl(static_cast<uint32_t>(off), row, kLanes);
-        bring(c, at, 0, row, buffer);
-      }
+      t.at = id * a.pool.block_stride + head_at + static_cast<uint64_t>(slot) * ts;
+      t.oks = __ballot(ok_next);
+      if constexpr (E4M3) scale_of(id, ok_next, t.f, t.lg, t.rc);
       look_up_1(tile + 1);
-    }
-  };
-  // e4m3: widens what fetch() has brought
-  const auto put = [&](uint32_t buffer) {
-    if constexpr (E4M3) {
-#pragma unroll
-      for (uint32_t c = 0; c < 2 * CHUNKS; ++c) {
-        const bool value = c >= CHUNKS;
-        const uint32_t row = (wave * CHUNKS + c % CHUNKS) * ROWS_A_CHUNK + lane / LANES_A_ROW;
-        TUTTI_LDS uint8_t *to = base + buffer * BUFFER + (value ? PLANE : 0) + row * ROW_BYTES;
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const u32x2 codes = {raw[c][2 * x], raw[c][2 * x + 1]};
-          const uint32_t unit = (2 * place + x) ^ swap_of<UNITS>(row);
-          u32x4 w;
-          if (value)
-            w = __builtin_bit_cast(u32x4, widen<Fp16>(codes));
-          else
-            w = __builtin_bit_cast(u32x4, widen<T>(codes));
-          *(TUTTI_LDS u32x4 *)(to + unit * 16) = w;
-        }
-      }
     }
   };
 
@@ -878,44 +876,86 @@ __global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const A
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
     const uint32_t j = lane & 15u, row = 8 * c + 4 * hf + j / 4, unit = 2 * (lane >> 4 & 1u) + (j & 3u) / 2;
-    value_at[c] = PLANE + row * ROW_BYTES + (unit ^ swap_of<UNITS>(row)) * 16 + (j & 1u) * 8;
+    value_at[c] = row * ROW_BYTES + (unit ^ swap_of<UNITS>(row)) * 16 + (j & 1u) * 8;
   }
   // keys 16x.. of the tile, values 32n..: what the products take
   const auto values_of = [&](uint32_t from, int n, int x) {
     s16x4 v[2];
 #pragma unroll
     for (int c = 0; c < 2; ++c)
-      v[c] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(in_lds<s16x4>(((from + value_at[c]) ^ (n << 6)) + 16 * x * ROW_BYTES));
+      v[c] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(in_lds<s16x4>(((lds_at + from + value_at[c]) ^ (n << 6)) + 16 * x * ROW_BYTES));
     return __builtin_bit_cast(typename P::eight, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
   };
   // which keys of a tile a lane's row sees: bit c for key c + 4*hf of it
-  const auto seen_of = [&](int t, uint32_t key0) {
-    const uint32_t from = lo[t] > key0 ? min(lo[t] - key0, kWideTile) : 0, to = hi[t] > key0 ? min(hi[t] - key0, kWideTile) : 0;
+  const auto seen_of = [&](uint32_t key0) {
+    const uint32_t from = lo > key0 ? min(lo - key0, kWideTile) : 0, to = hi > key0 ? min(hi - key0, kWideTile) : 0;
     uint64_t bits = now.oks;
     bits &= from < 64 ? ~0ull << from : 0;
     bits &= to < 64 ? ~(~0ull << to) : ~0ull;
     return bits >> (4 * hf);
   };
+  // Products of a tile's scores: step i of 2*STEPS is 16 values of the first or the second 32 keys, in turn.
+  const auto key_of = [&](uint32_t k_at, int i) {
+    return __builtin_bit_cast(typename T::eight, *in_lds<u32x4>(((lds_at + k_at + key_at) ^ (i / 2 << 5)) + i % 2 * 32 * ROW_BYTES));
+  };
+  // LDS: keys of even and of odd tiles, then the values
+  const auto k_of = [&](uint32_t tile) { return (tile - t0 & 1u) * PLANE; };
+  const auto v_of = [&](uint32_t tile) { return (2 + (tile - t0 & 1u)) * PLANE; };
+  // the tiles that some row of the wavefront sees
+  const uint32_t w_t0 = has_rows ? max(t0, w_any_lo / kWideTile) : t1;
+  const uint32_t w_t1 = has_rows ? min(t1, (w_any_hi + kWideTile - 1) / kWideTile) : 0;
 
+  // reads of LDS that are under way before the product that takes the first of them: of keys, of values, and of those between the
+  // products of the keys already (e4m3 has fewer registers left: the rows that come in are there too)
+  constexpr int AHEAD = 4, VALUES_AHEAD = DT, VALUES_EARLY = DT;
+  f32x16 sc[2];
+  const auto scores_alone = [&](uint32_t tile) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[h][i] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 2 * STEPS; ++i) sc[i % 2] = wide_product<T>(key_of(k_of(tile), i), q[i / 2], sc[i % 2]);
+  };
+
+  // Before tile t is worked on its scores are there, its values and the next tile's keys are in LDS; while it is worked on the next
+  // tile's values and the keys of the one after that come in.
   if (t1 > t0) {
-    if (!PAGED16) look_up_1(t0);
-    fetch(t0, 0);
-    put(0);
-  }
-  for (uint32_t tile = t0; tile < t1; ++tile) {
-    const uint32_t buffer = (tile - t0) & 1u, key0 = tile * kWideTile;
+    if (PAGED16)
+      look_up_16(t0);
+    else
+      look_up_1(t0);
+    find(t0, now);
+    bring(a.pool.k, t0, now, k_of(t0), raw_k);
+    bring(a.pool.v, t0, now, v_of(t0), raw_v);
+    put(k_of(t0), raw_k, T{});
+    put(v_of(t0), raw_v, Fp16{});
+    if (t0 + 1 < t1) {
+      find(t0 + 1, next);
+      bring(a.pool.k, t0 + 1, next, k_of(t0 + 1), raw_k);
+      put(k_of(t0 + 1), raw_k, T{});
+    }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    now = next;
-    const bool more = tile + 1 < t1;
-    if (E4M3 && !PAGED16) {
-      per_key[wave][0][lane] = now.f[0];
-      per_key[wave][1][lane] = now.lg[0];
-      per_key[wave][2][lane] = now.rc[0];
+    if (w_t0 == t0 && w_t1 > t0) scores_alone(t0);
+  }
+  for (uint32_t tile = t0; tile < t1; ++tile) {
+    const uint32_t key0 = tile * kWideTile, v_at = v_of(tile), k_at = k_of(tile + 1);
+    if (tile != t0) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
     }
-    if (more) fetch(tile + 1, buffer ^ 1u);
-    TUTTI_LDS uint8_t *const here = base + buffer * BUFFER;
-    const uint32_t here_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(here));
+    const bool more = tile + 1 < t1, more_keys = tile + 2 < t1;
+    if (E4M3 && !PAGED16) {
+      per_key[wave][0][lane] = now.f;
+      per_key[wave][1][lane] = now.lg;
+      per_key[wave][2][lane] = now.rc;
+    }
+    if (more) bring(a.pool.v, tile + 1, next, v_of(tile + 1), raw_v);
+    if (more_keys) {
+      find(tile + 2, second);
+      bring(a.pool.k, tile + 2, second, k_of(tile + 2), raw_k);
+    }
     const bool wg_edge = key0 < all_lo || key0 + kWideTile > all_hi || now.oks != ~0ull;
     bool odd = false;
     if (wg_edge) {
@@ -926,7 +966,7 @@ __global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const A
 #pragma unroll
       for (uint32_t x = 0; x < EACH; ++x) {
         const uint32_t unit = threadIdx.x * EACH + x, row = unit / UNITS;
-        TUTTI_LDS u32x4 *at = (TUTTI_LDS u32x4 *)(here + PLANE + unit * 16);
+        TUTTI_LDS u32x4 *at = (TUTTI_LDS u32x4 *)(base + v_at + unit * 16);
         u32x4 w = *at;
         if (!(now.oks >> row & 1u)) w = u32x4{0, 0, 0, 0};
 #pragma unroll
@@ -937,122 +977,121 @@ __global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const A
         }
         *at = w;
       }
-      odd = __syncthreads_or(any);
+      if (__ballot(any) && lane == 0) not_finite[wave] = 1;
+      __syncthreads();
+      odd = not_finite[0] | not_finite[1] | not_finite[2] | not_finite[3];
     }
-    if (has_rows && key0 < w_any_hi && key0 + kWideTile > w_any_lo) {
-      const bool edge = key0 < w_all_lo || key0 + kWideTile > w_all_hi || now.oks != ~0ull;
-      typename P::eight p[RW][4];
-      f32x16 sc[RW][2];
-      {
-        // the reads of half the keys are under way before the first product, those of the others while it goes on
-        u32x4 k[2][STEPS];
-        const auto read = [&](int h, int from, int to) {
+    if (tile >= w_t0 && tile < w_t1) {
+      typename T::eight k[2 * STEPS];
 #pragma unroll
-          for (int j = from; j < to; ++j) k[h][j] = *in_lds<u32x4>(((here_at + key_at) ^ (j << 5)) + h * 32 * ROW_BYTES);
-          __builtin_amdgcn_sched_barrier(0);
-        };
-        const auto multiply = [&](int h, int from, int to) {
-#pragma unroll
-          for (int j = from; j < to; ++j)
-#pragma unroll
-            for (int t = 0; t < RW; ++t) sc[t][h] = wide_product<T>(__builtin_bit_cast(typename T::eight, k[h][j]), q[t][j], sc[t][h]);
-          __builtin_amdgcn_sched_barrier(0);
-        };
-        read(0, 0, STEPS);
+      for (int i = 0; i < AHEAD; ++i) k[i] = key_of(k_at, i);
+      if (E4M3 && !PAGED16) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int t = 0; t < RW; ++t)
+          for (int i = 0; i < 16; i += 4) {
+            const f32x4 f = *reinterpret_cast<const f32x4 *>(&per_key[wave][0][32 * h + 2 * i + 4 * hf]);
+            const f32x4 lg = *reinterpret_cast<const f32x4 *>(&per_key[wave][1][32 * h + 2 * i + 4 * hf]);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sc[t][h][i] = 0.0f;
-        read(1, 0, STEPS / 2);
-        __builtin_amdgcn_s_setprio(1);  // the other wavefront's arithmetic fits between matrix instructions, not the other way round
-        multiply(0, 0, STEPS / 2);
-        read(1, STEPS / 2, STEPS);
-        multiply(0, STEPS / 2, STEPS);
-        multiply(1, 0, STEPS);
-        __builtin_amdgcn_s_setprio(0);
-      }
-      typename P::eight v[2][DT];  // of the 16 keys whose turn it is, and of the next
-#pragma unroll
-      for (int n = 0; n < DT; ++n) v[0][n] = values_of(here_at, n, 0);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int t = 0; t < RW; ++t) {
-        if (E4M3 && !PAGED16) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-              const f32x4 f = *reinterpret_cast<const f32x4 *>(&per_key[wave][0][32 * h + 2 * i + 4 * hf]);
-              const f32x4 lg = *reinterpret_cast<const f32x4 *>(&per_key[wave][1][32 * h + 2 * i + 4 * hf]);
-#pragma unroll
-              for (int x = 0; x < 4; ++x) sc[t][h][i + x] = sc[t][h][i + x] * f[x] + lg[x];
-            }
-        }
-        if (edge) {
-          asm volatile("" ::);  // (a branch: most tiles are whole ones)
-          const uint64_t seen = seen_of(t, key0);
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (!(seen >> (32 * h + 8 * (i / 4) + i % 4) & 1u)) sc[t][h][i] = -__builtin_inff();
-        }
-        // the largest of each 16 keys, then with their factors of all
-        float top = kLowest;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          float most = sc[t][x / 2][8 * (x & 1)];
-#pragma unroll
-          for (int i = 1; i < 8; ++i) most = fmaxf(most, sc[t][x / 2][8 * (x & 1) + i]);
-          if constexpr (E4M3 && PAGED16) most = most * now.f[x] + now.lg[x];
-          top = fmaxf(top, most);
-        }
-        if (!E4M3) top *= factor;
-        top = max_of_halves(top);
-        if (__ballot(top > m[t] + kRaise)) {
-          const float raised = top > m[t] + kRaise ? top : m[t];
-          const float by = __builtin_amdgcn_exp2f(m[t] - raised);
-          m[t] = raised;
-          l[t] *= by;
-#pragma unroll
-          for (int n = 0; n < DT; ++n) o[t][n] *= by;
-        }
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const float f = E4M3 ? (PAGED16 ? now.f[x] : 1.0f) : factor, less = (E4M3 && PAGED16 ? now.lg[x] : 0.0f) - m[t];
-          float sum = 0.0f;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][x / 2][8 * (x & 1) + i], f, less));
-            if constexpr (E4M3 && !PAGED16)
-              sum += w * per_key[wave][2][16 * x + 8 * (i / 4) + 4 * hf + i % 4];
-            else
-              sum += w;
-            p[t][x][i] = static_cast<typename P::one>(w);
+            for (int x = 0; x < 4; ++x) sc[h][i + x] = sc[h][i + x] * f[x] + lg[x];
           }
-          l[t] += E4M3 && PAGED16 ? sum * now.rc[x] : sum;
-        }
       }
+      if (key0 < w_all_lo || key0 + kWideTile > w_all_hi || now.oks != ~0ull) {
+        asm volatile("" ::);  // (a branch: most tiles are whole ones)
+        const uint64_t seen = seen_of(key0);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (!(seen >> (32 * h + 8 * (i / 4) + i % 4) & 1u)) sc[h][i] = -__builtin_inff();
+      }
+      float f16[4], lg16[4], rc16[4];  // e4m3, PAGED16: of each 16 keys
+      if constexpr (E4M3 && PAGED16)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const uint32_t from = (tile - looked.tile) * 4 + x;
+          f16[x] = __uint_as_float(from_lane(__float_as_uint(looked.f), from));
+          lg16[x] = __uint_as_float(from_lane(__float_as_uint(looked.lg), from));
+          rc16[x] = __uint_as_float(from_lane(__float_as_uint(looked.rc), from));
+        }
+      // the largest of each 16 keys, then with their factors of all
+      float top = kLowest;
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        if (x < 3)
+        float most = sc[x / 2][8 * (x & 1)];
 #pragma unroll
-          for (int n = 0; n < DT; ++n) v[(x + 1) & 1][n] = values_of(here_at, n, x + 1);
-        __builtin_amdgcn_sched_barrier(0);
-        if (x == 0) __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-        for (int n = 0; n < DT; ++n)
-#pragma unroll
-          for (int t = 0; t < RW; ++t) o[t][n] = wide_product<P>(v[x & 1][n], p[t][x], o[t][n]);
+        for (int i = 1; i < 8; ++i) most = fmaxf(most, sc[x / 2][8 * (x & 1) + i]);
+        if constexpr (E4M3 && PAGED16) most = most * f16[x] + lg16[x];
+        top = fmaxf(top, most);
       }
+      if (!E4M3) top *= factor;
+      top = max_of_halves(top);
+      if (__ballot(top > m + kRaise)) {
+        const float raised = top > m + kRaise ? top : m;
+        const float by = __builtin_amdgcn_exp2f(m - raised);
+        m = raised;
+        l *= by;
+#pragma unroll
+        for (int n = 0; n < DT; ++n) o[n] *= by;
+      }
+      // this tile's weights, two at a time, between the products of the next one's scores (of what lies there, if there is none:
+      // nobody asks for them)
+      typename P::eight p[4];
+      f32x16 following[2];
+      typename P::eight v[4 * DT];
+      float sum = 0.0f;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) following[h][i] = 0.0f;
+#pragma unroll
+      for (int y = 0; y < 16; ++y) {
+#pragma unroll
+        for (int i = y * 2 * STEPS / 16; i < (y + 1) * 2 * STEPS / 16; ++i) {
+          if (i + AHEAD < 2 * STEPS) k[i + AHEAD] = key_of(k_at, i + AHEAD);
+          following[i % 2] = wide_product<T>(k[i], q[i / 2], following[i % 2]);
+        }
+        if (y >= 16 - VALUES_EARLY) v[y - (16 - VALUES_EARLY)] = values_of(v_at, y - (16 - VALUES_EARLY), 0);
+        const int x = y / 4;
+        const float f = E4M3 ? (PAGED16 ? f16[x] : 1.0f) : factor, less = (E4M3 && PAGED16 ? lg16[x] : 0.0f) - m;
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          const int i = (2 * y + z) % 8;
+          const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x / 2][8 * (x & 1) + i], f, less));
+          if constexpr (E4M3 && !PAGED16)
+            sum += w * per_key[wave][2][16 * x + 8 * (i / 4) + 4 * hf + i % 4];
+          else
+            sum += w;
+          p[x][i] = static_cast<typename P::one>(w);
+        }
+        if (y % 4 == 3) {
+          l += E4M3 && PAGED16 ? sum * rc16[x] : sum;
+          sum = 0.0f;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      __builtin_amdgcn_s_setprio(1);  // the other wavefront's arithmetic fits between matrix instructions, not the other way round
+#pragma unroll
+      for (int i = VALUES_EARLY; i < VALUES_AHEAD; ++i) v[i] = values_of(v_at, i % DT, i / DT);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < 4 * DT; ++i) {
+        const int soon = i + VALUES_AHEAD;
+        if (soon < 4 * DT) v[soon] = values_of(v_at, soon % DT, soon / DT);
+        o[i % DT] = wide_product<P>(v[i], p[i / DT], o[i % DT]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) sc[h] = following[h];
+    } else if (tile + 1 == w_t0 && more) {
+      scores_alone(tile + 1);
     }
-    __builtin_amdgcn_s_setprio(0);
     if (odd) {
       // the infinities and NaN of the tile as numbers that say what they are, for the rows that see them: 1, 2^7 and 2^14, sums of
       // 64 of which say which there were
       __syncthreads();
+      if (threadIdx.x < 4) not_finite[threadIdx.x] = 0;  // (all have read it before they met here)
 #pragma unroll 1
       for (uint32_t x = threadIdx.x; x < PLANE / 16; x += 256) {
         const uint32_t row = x / UNITS, d0 = ((x % UNITS) ^ swap_of<UNITS>(row)) * 8, key = key0 + row;
@@ -1070,50 +1109,45 @@ __global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const A
             }
           }
         }
-        *(TUTTI_LDS u32x4 *)(here + PLANE + x * 16) = __builtin_bit_cast(u32x4, w);
+        *(TUTTI_LDS u32x4 *)(base + v_at + x * 16) = __builtin_bit_cast(u32x4, w);
       }
       __syncthreads();
       if (has_rows) {
+        const uint64_t bits = seen_of(key0);
 #pragma unroll
         for (int n = 0; n < DT; ++n) {
-          f32x16 sums[RW];
+          f32x16 sums;
 #pragma unroll
-          for (int t = 0; t < RW; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) sums[t][i] = 0.0f;
+          for (int i = 0; i < 16; ++i) sums[i] = 0.0f;
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            const typename P::eight v = values_of(here_at, n, x);
+            const typename P::eight v = values_of(v_at, n, x);
+            typename P::eight seen;
 #pragma unroll
-            for (int t = 0; t < RW; ++t) {
-              const uint64_t bits = seen_of(t, key0);
-              typename P::eight seen;
-#pragma unroll
-              for (int i = 0; i < 8; ++i) seen[i] = static_cast<typename P::one>(bits >> (16 * x + 8 * (i / 4) + i % 4) & 1u ? 1.0f : 0.0f);
-              sums[t] = wide_product<P>(v, seen, sums[t]);
-            }
+            for (int i = 0; i < 8; ++i) seen[i] = static_cast<typename P::one>(bits >> (16 * x + 8 * (i / 4) + i % 4) & 1u ? 1.0f : 0.0f);
+            sums = wide_product<P>(v, seen, sums);
           }
 #pragma unroll
-          for (int t = 0; t < RW; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const uint32_t which = static_cast<uint32_t>(sums[t][i]);
+          for (int i = 0; i < 16; ++i) {
+              const uint32_t which = static_cast<uint32_t>(sums[i]);
               const bool up = which & 0x7fu, down = which >> 7 & 0x7fu, none = which >> 14;
-              if (which) o[t][n][i] += none || (up && down) ? __builtin_nanf("") : up ? __builtin_inff() : -__builtin_inff();
+              if (which) o[n][i] += none || (up && down) ? __builtin_nanf("") : up ? __builtin_inff() : -__builtin_inff();
             }
         }
       }
     }
-    if (more) put(buffer ^ 1u);
+    if (more) put(v_of(tile + 1), raw_v, Fp16{});
+    if (more_keys) put(k_of(tile + 2), raw_k, T{});
+    now = next;
+    next = second;
   }
-  if (__ballot(skipped) && lane == 0) report(a.status, TUTTI_ST_BAD_BLOCK);
+  if (skipped && lane == 0) report(a.status, TUTTI_ST_BAD_BLOCK);
   __syncthreads();  // LDS changes hands: from here each wavefront has a part of it
   const AttendArgs &z = arguments_again<AttendArgs>();
 
-#pragma unroll
-  for (int t = 0; t < RW; ++t) {
-    const float sum = sum_of_halves(l[t]);
-    const uint32_t row_in = wave * 32 * RW + t * 32 + r, row = row_a + row_in;
+  {
+    const float sum = sum_of_halves(l);
+    const uint32_t row_in = wave * 32 + r, row = row_a + row_in;
     if (u.parts > 1) {
       if (row < n_rows) {
         const uint64_t at = static_cast<uint64_t>(u.part_slot + u.part) * ROWS + row_in;
@@ -1122,10 +1156,10 @@ __global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const A
 #pragma unroll
           for (int i = 0; i < 16; i += 4)
             *reinterpret_cast<f32x4 *>(z.part_o + at * DP + 32 * n + 2 * i + 4 * hf) =
-                f32x4{o[t][n][i], o[t][n][i + 1], o[t][n][i + 2], o[t][n][i + 3]};
-        if (hf == 0) z.part_ml[at] = f32x2{m[t], sum};
+                f32x4{o[n][i], o[n][i + 1], o[n][i + 2], o[n][i + 3]};
+        if (hf == 0) z.part_ml[at] = f32x2{m, sum};
       }
-      continue;
+      return;
     }
     // through LDS, so that whole rows are stored
     constexpr uint32_t OUT_BYTES = ROW_BYTES + 16;
@@ -1138,8 +1172,8 @@ __global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const A
         typename T::two two[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          two[x][0] = static_cast<typename T::one>(o[t][n][i + 2 * x] * by);
-          two[x][1] = static_cast<typename T::one>(o[t][n][i + 2 * x + 1] * by);
+          two[x][0] = static_cast<typename T::one>(o[n][i + 2 * x] * by);
+          two[x][1] = static_cast<typename T::one>(o[n][i + 2 * x + 1] * by);
         }
         *(TUTTI_LDS u32x2 *)(mine + r * OUT_BYTES + (32 * n + 2 * i + 4 * hf) * 2) =
             u32x2{__builtin_bit_cast(uint32_t, two[0]), __builtin_bit_cast(uint32_t, two[1])};
@@ -1147,19 +1181,17 @@ __global__ __launch_bounds__(256, RW == 1 ? 2 : 1) void k_kv_attend_wide(const A
     if (row < n_rows && hf == 0 && z.lse) {
       const uint32_t i = row / z.group, head = u.head * z.group + row - i * z.group;
       z.lse[static_cast<uint64_t>(s.row0 + i) * (z.kv_heads * z.group) + head] =
-          sum == 0.0f ? -__builtin_inff() : (m[t] + __builtin_amdgcn_logf(sum)) * kLn2;
+          sum == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(sum)) * kLn2;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
     for (uint32_t x = lane; x < 32 * UNITS; x += kLanes) {
-      const uint32_t in = x / UNITS, unit = x % UNITS, out_row = wave_a + t * 32 + in;
+      const uint32_t in = x / UNITS, unit = x % UNITS, out_row = wave_a + in;
       if (out_row >= n_rows || unit * 8 >= d) continue;
       const uint32_t i = out_row / z.group, head = u.head * z.group + out_row - i * z.group;
       *reinterpret_cast<u32x4 *>(static_cast<uint8_t *>(z.out.base) + static_cast<uint64_t>(s.row0 + i) * z.out.row_stride +
                                  head * z.out.head_stride + unit * 16) = *(TUTTI_LDS u32x4 *)(mine + in * OUT_BYTES + unit * 16);
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
   }
 }
 
