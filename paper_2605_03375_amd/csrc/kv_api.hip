@@ -118,6 +118,11 @@ uint32_t rows_a_tile(const tutti_batch *b, uint32_t group) {
   return most <= 16 ? 16 : most <= 32 ? 32 : 128;
 }
 
+// Workgroups of an attention kernel that the device is taken to hold at once: two a compute unit.  (The kernels for few rows would fit
+// three times; 128K tokens of one sequence: 61.7 us with 512, 66.7 with 768, whose parts take longer to join.)  The size of the work
+// memory goes by it, so it does not go by the device.
+constexpr uint32_t kAttendSlots = 512;
+
 // Neighbouring KV heads that a workgroup takes side by side, so that it reads stretches of a block and not a head's rows here and
 // there (128-byte rows of 8 heads: 4.7 TB/s one head a workgroup, 5.8 with four side by side, 6.0 with eight).
 uint32_t heads_abreast(uint32_t kv_heads) {
@@ -127,12 +132,10 @@ uint32_t heads_abreast(uint32_t kv_heads) {
 }
 
 struct AttendSizes {
-  uint32_t rows, dp, abreast, key_waves, target, max_units, max_parts;
+  uint32_t rows, dp, abreast, key_waves, slots, min_tiles, max_units, max_parts;
   uint64_t ml_bytes, bytes;
 };
 
-// Parts that the keys of all sequences are split into come to at most 2 * target (a sequence is split only if it has more
-// tiles than one part takes), units to at most target + the row tiles that there can be.
 int attend_sizes(const tutti_pool *pool, const tutti_batch *b, const tutti_attn *attn, AttendSizes *s) {
   const uint32_t group = attn->n_q_heads / pool->num_kv_heads;
   s->rows = rows_a_tile(b, group);
@@ -140,18 +143,23 @@ int attend_sizes(const tutti_pool *pool, const tutti_batch *b, const tutti_attn 
   if (s->rows < 128) {
     s->abreast = heads_abreast(pool->num_kv_heads);
     s->key_waves = s->abreast == 1 ? 4 : s->abreast == 2 ? 2 : 1;
-    s->target = 768;  // three workgroups a compute unit: what fits of most kernels
   } else {
     s->abreast = s->key_waves = 1;
-    s->target = 512;
   }
+  s->slots = kAttendSlots;
+  // fewer tiles than this a part are not worth their join (32K tokens: parts of 8 tiles 34.4 us, of 4 tiles 36.9; 512 tokens, where
+  // two wavefronts share a part: of 4 tiles 11.2, of 8 tiles 12.4)
+  s->min_tiles = s->key_waves == 1 ? 8 : 4;
+  // Units: two rounds of the slots at most or, with an even share a part, a round of them and one more for every row tile.  Parts of
+  // sequences that are split: the same two rounds; with an even share a split sequence's row tiles have more tiles than a share
+  // each, so that they are no more than a round, and their parts no more than two.
   const uint64_t tiles = static_cast<uint64_t>(b->n_rows) * group / s->rows + std::min(b->n_seq, b->n_rows);
-  const uint64_t units = s->target + tiles * (pool->num_kv_heads / s->abreast);
+  const uint64_t units = 2 * s->slots + tiles * (pool->num_kv_heads / s->abreast);
   if (units >= 0x80000000ull || static_cast<uint64_t>(b->n_rows) * attn->n_q_heads >= 0x80000000ull) return TUTTI_ERANGE;
   s->max_units = static_cast<uint32_t>(units);
-  s->max_parts = 2 * s->target * s->abreast;
+  s->max_parts = 2 * s->slots * s->abreast;
   s->ml_bytes = static_cast<uint64_t>(s->max_parts) * s->rows * sizeof(f32x2);
-  s->bytes = s->ml_bytes + static_cast<uint64_t>(s->max_parts) * s->rows * s->dp * sizeof(float);
+  s->bytes = 16 + s->ml_bytes + static_cast<uint64_t>(s->max_parts) * s->rows * s->dp * sizeof(float);
   return TUTTI_OK;
 }
 
@@ -326,12 +334,13 @@ int tutti_kv_attend(const tutti_pool *pool, const tutti_scales *scales, const tu
   a.window = attn->window;
   a.abreast = s.abreast;
   a.key_waves = s.key_waves;
-  a.target = s.target;
-  a.min_tiles = 8;
+  a.slots = s.slots;
+  a.min_tiles = s.min_tiles;
   a.max_units = s.max_units;
   a.max_parts = s.max_parts;
-  a.part_ml = static_cast<f32x2 *>(d_work);
-  a.part_o = reinterpret_cast<float *>(static_cast<uint8_t *>(d_work) + s.ml_bytes);
+  a.tiles_a_part = static_cast<uint32_t *>(d_work);
+  a.part_ml = reinterpret_cast<f32x2 *>(static_cast<uint8_t *>(d_work) + 16);
+  a.part_o = reinterpret_cast<float *>(static_cast<uint8_t *>(d_work) + 16 + s.ml_bytes);
   a.status = d_status;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   if (attn->dtype == TUTTI_BF16)

@@ -23,18 +23,15 @@ struct AttendArgs {
   uint32_t abreast, key_waves;
   float scale_log2;             // sm_scale * log2(e)
   uint32_t causal, window;
-  // How the keys are split: a sequence's tiles go in parts of about max(min_tiles, all tiles / target) tiles.
-  uint32_t target, min_tiles, max_units, max_parts;
+  // How the keys are split (make_plan): workgroups that the device holds at once, the fewest tiles of a part, and what there can be.
+  uint32_t slots, min_tiles, max_units, max_parts;
+  uint32_t *tiles_a_part;       // what the attention kernel has chosen, for the join
   float *part_o;                // [part][rows][dp]: sums of weighted values
   f32x2 *part_ml;               // [part][rows]: running maximum (log2) and sum of weights
   uint32_t *status;
 };
 
-// What a step's sequences come to.  Rows: new tokens times query heads of a KV head, in tiles of RT*16.
-struct Plan {
-  uint32_t tiles_a_part;
-};
-
+// Rows of a sequence: new tokens times query heads of a KV head, in tiles of ROWS.
 template <int ROWS>
 __device__ __forceinline__ uint32_t row_tiles(const AttendArgs &a, const tutti_seq &s) {
   return (s.n_new * a.group + ROWS - 1) / ROWS;
@@ -49,29 +46,80 @@ __device__ __forceinline__ uint32_t key_tiles(const AttendArgs &a, const tutti_s
   return (s.n_held + kKeyTile - 1) / kKeyTile - first_key(a, s) / kKeyTile;
 }
 
-template <int ROWS>
-__device__ __forceinline__ Plan make_plan(const AttendArgs &a) {
-  const uint32_t lane = threadIdx.x & (kLanes - 1);
-  uint64_t work = 0;
-  for (uint32_t base = 0; base < a.batch.n_seq; base += kLanes) {
-    if (base + lane < a.batch.n_seq) {
-      const tutti_seq s = load_seq(a.batch.seqs + base + lane);
-      if (seq_ok(a.batch, s) && s.n_new) work += static_cast<uint64_t>(row_tiles<ROWS>(a, s)) * key_tiles(a, s);
-    }
-  }
-#pragma unroll
-  for (int m = 1; m < static_cast<int>(kLanes); m <<= 1) work += __shfl_xor(work, m, kLanes);
-  work *= a.kv_heads / a.abreast;
-  const uint64_t each = (work + a.target - 1) / a.target;
-  Plan p;
-  p.tiles_a_part = uniform(each > 0x40000000u ? 0x40000000u : static_cast<uint32_t>(each));
-  if (p.tiles_a_part < a.min_tiles) p.tiles_a_part = a.min_tiles;
-  return p;
-}
+// How many tiles a part of the keys has.  Every workgroup works this out from the records, which costs less than a launch before it.
+struct Plan {
+  uint32_t tiles_a_part;
+  tutti_seq lane_seq;  // record `lane` of the first 64: read once
+};
 
 __device__ __forceinline__ uint32_t parts_of(const AttendArgs &a, const Plan &p, const tutti_seq &s) {
   const uint32_t n = (key_tiles(a, s) + p.tiles_a_part - 1) / p.tiles_a_part;
   return n ? n : 1;
+}
+
+__device__ __forceinline__ tutti_seq record(const AttendArgs &a, const Plan &p, uint32_t base, uint32_t lane) {
+  return base ? load_seq(a.batch.seqs + base + lane) : p.lane_seq;
+}
+
+// A part has the tiles that make the parts fill the device's slots once or, where that goes up better, twice: with one part more than
+// slots the last one has them for itself (32 sequences, 516 parts for 512 slots: 56 us, 488 parts: 42).  What is weighed is rounds times
+// (tiles of a part + kUnitTiles, what a workgroup costs beside its tiles).  More than 64 sequences, or more row tiles than two
+// rounds have slots for: an even share of all tiles, which leaves most sequences whole.
+constexpr uint32_t kUnitTiles = 8;
+
+template <int ROWS>
+__device__ __forceinline__ Plan make_plan(const AttendArgs &a) {
+  const uint32_t lane = threadIdx.x & (kLanes - 1), head_groups = a.kv_heads / a.abreast;
+  Plan p{};
+  if (lane < a.batch.n_seq) p.lane_seq = load_seq(a.batch.seqs + lane);
+  uint64_t work = 0;
+  uint32_t rows = 0, tiles = 0;  // of the lane's last sequence
+  for (uint32_t base = 0; base < a.batch.n_seq; base += kLanes) {
+    if (base + lane < a.batch.n_seq) {
+      const tutti_seq s = record(a, p, base, lane);
+      if (seq_ok(a.batch, s) && s.n_new) {
+        rows = row_tiles<ROWS>(a, s) * head_groups;
+        tiles = key_tiles(a, s);
+        work += static_cast<uint64_t>(rows) * tiles;
+      }
+    }
+  }
+#pragma unroll
+  for (int m = 1; m < static_cast<int>(kLanes); m <<= 1) work += __shfl_xor(work, m, kLanes);
+  const auto share = [&](uint32_t slots) {
+    const uint64_t each = (work + slots - 1) / slots;
+    const uint32_t most = 0x40000000u, n = each > most ? most : static_cast<uint32_t>(each);
+    return uniform(n < a.min_tiles ? a.min_tiles : n);
+  };
+  p.tiles_a_part = share(a.slots);
+  const uint32_t row_tiles_all = a.batch.n_seq > kLanes ? ~0u : from_lane(lane_prefix_sum(rows), kLanes - 1);
+  uint32_t best = ~0u;
+  for (uint32_t rounds = 1; rounds <= 2; ++rounds) {
+    const uint32_t limit = rounds * a.slots;
+    if (row_tiles_all == 0 || row_tiles_all > limit) continue;
+    uint32_t n;
+    bool fits = true;
+    if (a.batch.n_seq == 1) {
+      const uint32_t parts = limit / row_tiles_all;
+      n = uniform((from_lane(tiles, 0) + parts - 1) / parts);
+      if (n < a.min_tiles) n = a.min_tiles;
+    } else {
+      n = share(limit);
+      fits = false;
+      for (int x = 0; x < 6 && !fits; ++x) {
+        const uint32_t units = from_lane(lane_prefix_sum(rows * ((tiles + n - 1) / n)), kLanes - 1);
+        fits = units <= limit;
+        if (fits) break;
+        const uint32_t more = static_cast<uint32_t>(static_cast<float>(n) * static_cast<float>(units - limit) / static_cast<float>(limit));
+        n = uniform(n + (more ? more : 1));
+      }
+    }
+    if (fits && rounds * (n + kUnitTiles) < best) {
+      best = rounds * (n + kUnitTiles);
+      p.tiles_a_part = n;
+    }
+  }
+  return p;
 }
 
 // Where a unit's results go.
@@ -93,7 +141,7 @@ __device__ __forceinline__ Unit locate(const AttendArgs &a, const Plan &p, uint3
     tutti_seq s{};
     uint32_t n = 0, split = 0, tiles = 0, parts = 0;
     if (base + lane < a.batch.n_seq) {
-      s = load_seq(a.batch.seqs + base + lane);
+      s = record(a, p, base, lane);
       const bool ok = seq_ok(a.batch, s);
       bad |= !ok;
       if (ok && s.n_new) {
@@ -229,6 +277,7 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 ? 3 : 2) void k_kv_attend(
   const bool reporter = blockIdx.x == 0 && wave == 0;
   if (blockIdx.x >= a.max_units) return;
   const Plan plan = make_plan<ROWS>(a);
+  if (reporter && (threadIdx.x & (kLanes - 1)) == 0) *a.tiles_a_part = plan.tiles_a_part;
   const Unit u = locate<ROWS>(a, plan, blockIdx.x, reporter);
   if (u.seq == a.batch.n_seq) return;
   if (u.parts > 1 && u.part_slot + a.abreast * u.parts > a.max_parts) {
@@ -677,6 +726,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
   const bool reporter = blockIdx.x == 0 && wave == 0;
   if (blockIdx.x >= a.max_units) return;
   const Plan plan = make_plan<ROWS>(a);
+  if (reporter && (threadIdx.x & (kLanes - 1)) == 0) *a.tiles_a_part = plan.tiles_a_part;
   const Unit u = locate<ROWS>(a, plan, blockIdx.x, reporter);
   if (u.seq == a.batch.n_seq) return;
   if (u.parts > 1 && u.part_slot + u.parts > a.max_parts) {
@@ -1202,7 +1252,8 @@ __global__ __launch_bounds__(256) void k_kv_join(const AttendArgs a) {
   constexpr uint32_t TP = DP / 4, ABREAST = WAVES * kLanes / TP, U = 4;
   const uint32_t lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
   const uint32_t thread = WAVES == 4 ? threadIdx.x : lane;   // among those of the row
-  const Plan plan = make_plan<ROWS>(a);
+  Plan plan{*a.tiles_a_part, {}};
+  if (lane < a.batch.n_seq) plan.lane_seq = load_seq(a.batch.seqs + lane);
   // items: rows of the sequences that are split
   for (uint32_t item = WAVES == 4 ? blockIdx.x : blockIdx.x * 4 + uniform(wave);; item += gridDim.x * (4 / WAVES)) {
   uint32_t before = 0, slots = 0, units = 0;
@@ -1212,7 +1263,7 @@ __global__ __launch_bounds__(256) void k_kv_join(const AttendArgs a) {
     tutti_seq s{};
     uint32_t n = 0, split = 0, p = 0, all = 0;
     if (base + lane < a.batch.n_seq) {
-      s = load_seq(a.batch.seqs + base + lane);
+      s = record(a, plan, base, lane);
       if (seq_ok(a.batch, s) && s.n_new) {
         p = parts_of(a, plan, s);
         all = row_tiles<ROWS>(a, s) * (a.kv_heads / a.abreast) * p;
