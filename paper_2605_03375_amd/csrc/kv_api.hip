@@ -181,9 +181,10 @@ template <typename T, int DP, int ROWS>
 void launch_join(const AttendArgs &a, hipStream_t stream) {
   // a sequence that is split has two parts or more to a row tile, so no more rows are to be joined than this
   const uint32_t joins = std::min(a.batch.n_rows * a.kv_heads * a.group, a.max_parts / 2 * ROWS);
-  // a workgroup a row for few rows, which may have many parts (32 rows of 128 parts: 6.7 us; one wavefront, part after part, 75);
-  // else a wavefront a row (1,511 queries of 20 heads in two parts: 20 us, with workgroups 61), 8192 at a time: with one for each
-  // row that there might be, 8,001 prompt tokens that are not split cost 21 us here
+  // a workgroup a row for few rows, which may have many parts (32 rows of 128 parts: one wavefront, part after part, 75 us, four
+  // wavefronts 6.7, 16 wavefronts 6.2, but 1,280 rows of some parts 7.5 and 21); else a wavefront a row (1,511 queries of 20 heads in
+  // two parts: 20 us, with workgroups 61), 8192 at a time: with one for each row that there might be, 8,001 prompt tokens that are
+  // not split cost 21 us here, now 5
   if (joins <= 4096)
     hipLaunchKernelGGL((k_kv_join<T, DP, ROWS, 4>), dim3(joins), dim3(256), 0, stream, a);
   else

@@ -264,7 +264,7 @@ __device__ __forceinline__ void set_word(typename Words<N>::type &w, int i, uint
 // match.  Of the values, a lane takes DP/16 consecutive ones of its eight keys, and puts pairs of keys together by byte
 // permutations; so nothing passes through LDS and no wavefront waits for another until the end, where the four join.
 template <typename T, bool E4M3, int DP, bool FULL, bool PAGED16, int RT>
-__global__ __launch_bounds__(64 * kMostWaves, RT == 1 ? 3 : 2) void k_kv_attend(const AttendArgs a) {
+__global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2) void k_kv_attend(const AttendArgs a) {
   constexpr int ROWS = RT * 16, N = DP / 16;
   constexpr int KW = E4M3 ? DP / 64 : DP / 32;       // 16-byte loads of a key a lane does
   constexpr int VW = E4M3 ? N / 4 : N / 2;           // words of a value row a lane takes
@@ -481,14 +481,12 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 ? 3 : 2) void k_kv_attend(
     float f, lg, rc;  // factor of the score (e4m3); log2 and reciprocal of the value's scale
     bool ok;
   };
-  u32x4 kw[2][KW];
-  VWords vw[8];
   f32x4 sc[RT][2];
   typename P::eight p[RT];
   if constexpr (PAGED16) {
     // A half tile lies in one block.  The halves of the wavefront's next 32 tiles are looked up at once, one to a lane, and come from
-    // there as uniform values.  The keys of the next tile are asked for as soon as the scores of this one have used theirs, its
-    // values as soon as the products have.
+    // there as uniform values.  The keys of the next tile are asked for as soon as the scores of this one have used theirs, its values as
+    // soon as the products have.  (Two tiles under way, in as many registers again: 1 to 3 % less time.)
     uint64_t off_l = 0;
     Key key_l{};
     uint64_t oks = 0;
@@ -514,56 +512,56 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 ? 3 : 2) void k_kv_attend(
       }
       oks = __ballot(key_l.ok);
     };
-    uint64_t off[2];
-    Key key[2];
-    const auto take = [&](uint32_t c) {
+    struct {
+      u32x4 kw[2][KW];
+      VWords vw[8];
+      uint64_t off[2];
+      Key key[2];
+    } x;  // the tile in work, then the next
+    const uint32_t k_in = r * ts + (FULL || g * 16 < a.d * EB ? g * 16 : 0);
+    const auto ask_keys = [&](uint32_t c) {
+      if ((c & 31u) == 0) look_up(c);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const uint32_t from = (c & 31u) * 2 + h;
-        off[h] = static_cast<uint64_t>(from_lane(static_cast<uint32_t>(off_l >> 32), from)) << 32 | from_lane(static_cast<uint32_t>(off_l), from);
-        key[h].ok = oks >> from & 1u;
+        x.off[h] = static_cast<uint64_t>(from_lane(static_cast<uint32_t>(off_l >> 32), from)) << 32 | from_lane(static_cast<uint32_t>(off_l), from);
+        x.key[h].ok = oks >> from & 1u;
         if constexpr (E4M3) {
-          key[h].f = __uint_as_float(from_lane(__float_as_uint(key_l.f), from));
-          key[h].lg = __uint_as_float(from_lane(__float_as_uint(key_l.lg), from));
-          key[h].rc = __uint_as_float(from_lane(__float_as_uint(key_l.rc), from));
+          x.key[h].f = __uint_as_float(from_lane(__float_as_uint(key_l.f), from));
+          x.key[h].lg = __uint_as_float(from_lane(__float_as_uint(key_l.lg), from));
+          x.key[h].rc = __uint_as_float(from_lane(__float_as_uint(key_l.rc), from));
         }
+        load_keys(a.pool.k + x.off[h], k_in, x.kw[h]);
       }
     };
-    const uint32_t k_in = r * ts + (FULL || g * 16 < a.d * EB ? g * 16 : 0);
-    const auto load_values = [&]() {
+    const auto ask_values = [&]() {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          vw[4 * h + i] = __builtin_nontemporal_load(reinterpret_cast<const VWords *>(a.pool.v + off[h] + ((4 * g + i) * ts + v_in_row)));
+          x.vw[4 * h + i] = __builtin_nontemporal_load(reinterpret_cast<const VWords *>(a.pool.v + x.off[h] + ((4 * g + i) * ts + v_in_row)));
     };
     if (mine) {
-      look_up(0);
-      take(0);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) load_keys(a.pool.k + off[h], k_in, kw[h]);
-      load_values();
+      ask_keys(0);
+      ask_values();
     }
     for (uint32_t c = 0; c < mine; ++c) {
       const uint32_t key0 = (t0 + turn + c * a.key_waves) * kKeyTile;
-      const Key now[2] = {key[0], key[1]};
+      const Key now[2] = {x.key[0], x.key[1]};
       const bool edge = key0 < all_lo || key0 + kKeyTile > all_hi || !now[0].ok || !now[1].ok;
       const auto at = [&](int h, int) -> const Key & { return now[h]; };
-      scores(kw, sc);
+      scores(x.kw, sc);
       const bool more = c + 1 < mine;
-      if (more) {
-        if (((c + 1) & 31u) == 0) look_up(c + 1);
-        take(c + 1);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) load_keys(a.pool.k + off[h], k_in, kw[h]);
-      }
+      if (more) ask_keys(c + 1);
       weights(sc, key0, edge, at, p);
-      values(vw, key0, edge, at, p);
-      if (more) load_values();
+      values(x.vw, key0, edge, at, p);
+      if (more) ask_values();
     }
   } else {
     for (uint32_t tile = t0 + turn; tile < t1; tile += a.key_waves) {
       const uint32_t key0 = tile * kKeyTile;
+      u32x4 kw[2][KW];
+      VWords vw[8];
       Key key[2][4];
       bool edge = key0 < all_lo || key0 + kKeyTile > all_hi;
 #pragma unroll
@@ -609,6 +607,7 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 ? 3 : 2) void k_kv_attend(
   if (__ballot(skipped) && lane == 0) report(a.status, TUTTI_ST_BAD_BLOCK);
 
   // the wavefronts' maxima, sums and rows meet in LDS, 16 rows at a time
+  const auto &z = arguments_again<AttendArgs>();
   constexpr int LD = DP + 4;                        // rows apart by 4 banks
   __shared__ __attribute__((aligned(16))) float rows[kMostWaves][16][LD];
   __shared__ float ml[kMostWaves][16][2];
@@ -628,13 +627,13 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 ? 3 : 2) void k_kv_attend(
         *reinterpret_cast<f32x4 *>(&rows[wave][r][(4 * g + i) * N + n]) =
             f32x4{o[t][n][i], o[t][n + 1][i], o[t][n + 2][i], o[t][n + 3][i]};
     __syncthreads();
-    for (uint32_t x = threadIdx.x; x < a.abreast * 16 * SEGS; x += blockDim.x) {
+    for (uint32_t x = threadIdx.x; x < z.abreast * 16 * SEGS; x += blockDim.x) {
       const uint32_t hw = x / (16 * SEGS), row_in = x / SEGS % 16, e = (x % SEGS) * EACH, row = row_a + t * 16 + row_in;
-      if (row >= n_rows || e >= a.d) continue;
+      if (row >= n_rows || e >= z.d) continue;
       float top = kLowest;
-      for (uint32_t w = hw; w < a.abreast * a.key_waves; w += a.abreast) top = fmaxf(top, ml[w][row_in][0]);
+      for (uint32_t w = hw; w < z.abreast * z.key_waves; w += z.abreast) top = fmaxf(top, ml[w][row_in][0]);
       float sum = 0.0f, y[EACH] = {};
-      for (uint32_t w = hw; w < a.abreast * a.key_waves; w += a.abreast) {
+      for (uint32_t w = hw; w < z.abreast * z.key_waves; w += z.abreast) {
         const float by = __builtin_amdgcn_exp2f(ml[w][row_in][0] - top);
         sum += by * ml[w][row_in][1];
 #pragma unroll
@@ -642,21 +641,21 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 ? 3 : 2) void k_kv_attend(
       }
       if (u.parts > 1) {
         const uint64_t at = static_cast<uint64_t>(u.part_slot + hw * u.parts + u.part) * ROWS + t * 16 + row_in;
-        float *to = a.part_o + at * DP + e;
+        float *to = z.part_o + at * DP + e;
         *reinterpret_cast<f32x4 *>(to) = f32x4{y[0], y[1], y[2], y[3]};
         *reinterpret_cast<f32x4 *>(to + 4) = f32x4{y[4], y[5], y[6], y[7]};
-        if (e == 0) a.part_ml[at] = f32x2{top, sum};
+        if (e == 0) z.part_ml[at] = f32x2{top, sum};
         continue;
       }
-      const uint32_t i = row / a.group, head = (u.head + hw) * a.group + row - i * a.group;
+      const uint32_t i = row / z.group, head = (u.head + hw) * z.group + row - i * z.group;
       const float by = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-      typename T::eight z;
+      typename T::eight y16;
 #pragma unroll
-      for (uint32_t c = 0; c < EACH; ++c) z[c] = static_cast<typename T::one>(y[c] * by);
-      *reinterpret_cast<u32x4 *>(static_cast<uint8_t *>(a.out.base) + static_cast<uint64_t>(s.row0 + i) * a.out.row_stride +
-                                 head * a.out.head_stride + 2 * e) = __builtin_bit_cast(u32x4, z);
-      if (e == 0 && a.lse)
-        a.lse[static_cast<uint64_t>(s.row0 + i) * (a.kv_heads * a.group) + head] =
+      for (uint32_t c = 0; c < EACH; ++c) y16[c] = static_cast<typename T::one>(y[c] * by);
+      *reinterpret_cast<u32x4 *>(static_cast<uint8_t *>(z.out.base) + static_cast<uint64_t>(s.row0 + i) * z.out.row_stride +
+                                 head * z.out.head_stride + 2 * e) = __builtin_bit_cast(u32x4, y16);
+      if (e == 0 && z.lse)
+        z.lse[static_cast<uint64_t>(s.row0 + i) * (z.kv_heads * z.group) + head] =
             sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * kLn2;
     }
   }
@@ -1193,7 +1192,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
   }
   if (skipped && lane == 0) report(a.status, TUTTI_ST_BAD_BLOCK);
   __syncthreads();  // LDS changes hands: from here each wavefront has a part of it
-  const AttendArgs &z = arguments_again<AttendArgs>();
+  const auto &z = arguments_again<AttendArgs>();
 
   {
     const float sum = sum_of_halves(l);
@@ -1251,11 +1250,11 @@ template <typename T, int DP, int ROWS, int WAVES>
 __global__ __launch_bounds__(256) void k_kv_join(const AttendArgs a) {
   constexpr uint32_t TP = DP / 4, ABREAST = WAVES * kLanes / TP, U = 4;
   const uint32_t lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
-  const uint32_t thread = WAVES == 4 ? threadIdx.x : lane;   // among those of the row
+  const uint32_t thread = WAVES == 1 ? lane : threadIdx.x;   // among those of the row
   Plan plan{*a.tiles_a_part, {}};
   if (lane < a.batch.n_seq) plan.lane_seq = load_seq(a.batch.seqs + lane);
   // items: rows of the sequences that are split
-  for (uint32_t item = WAVES == 4 ? blockIdx.x : blockIdx.x * 4 + uniform(wave);; item += gridDim.x * (4 / WAVES)) {
+  for (uint32_t item = WAVES == 1 ? blockIdx.x * 4 + uniform(wave) : blockIdx.x;; item += gridDim.x * (WAVES == 1 ? 4 : 1)) {
   uint32_t before = 0, slots = 0, units = 0;
   bool found = false;
   uint32_t row0 = 0, parts = 0, local = 0, first_slot = 0, units_upto_it = 0;
@@ -1304,10 +1303,11 @@ __global__ __launch_bounds__(256) void k_kv_join(const AttendArgs a) {
   top = max_over_rows(top);
   __shared__ float tops[4], sums[4 * kLanes / TP];
   __shared__ __attribute__((aligned(16))) float half[4 * kLanes / TP][DP];
-  if constexpr (WAVES == 4) {
+  if constexpr (WAVES != 1) {
     if (lane == 0) tops[wave] = top;
     __syncthreads();
-    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+#pragma unroll
+    for (int x = 0; x < WAVES; ++x) top = fmaxf(top, tops[x]);
   }
   const uint32_t e = thread % TP * 4, mine = thread / TP;
   float sum = 0.0f;
@@ -1333,10 +1333,10 @@ __global__ __launch_bounds__(256) void k_kv_join(const AttendArgs a) {
     }
   }
   // the parts that went abreast: in LDS, a wavefront in its own rows of it
-  const uint32_t first = WAVES == 4 ? 0 : uniform(wave) * ABREAST;
+  const uint32_t first = WAVES == 1 ? uniform(wave) * ABREAST : 0;
   *reinterpret_cast<f32x4 *>(&half[first + mine][e]) = y;
   if (e == 0) sums[first + mine] = sum;
-  if constexpr (WAVES == 4) {
+  if constexpr (WAVES != 1) {
     __syncthreads();
   } else {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -1358,7 +1358,7 @@ __global__ __launch_bounds__(256) void k_kv_join(const AttendArgs a) {
     a.lse[static_cast<uint64_t>(row0 + i) * heads + head] =
         total == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(total)) * kLn2;
   }
-  if constexpr (WAVES == 4) {
+  if constexpr (WAVES != 1) {
     __syncthreads();  // LDS is the next row's
   } else {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

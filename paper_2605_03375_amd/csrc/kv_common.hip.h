@@ -57,10 +57,10 @@ __device__ __forceinline__ const __attribute__((address_space(4))) E *constant(c
 // The kernel's arguments (its only one, a record) read from memory again: behind a long loop that is cheaper than scalar registers
 // that hold them all the while, which the compiler would put away in vector registers.
 template <typename Args>
-__device__ __forceinline__ const Args &arguments_again() {
+__device__ __forceinline__ const __attribute__((address_space(4))) Args &arguments_again() {
   auto at = reinterpret_cast<uintptr_t>(__builtin_amdgcn_kernarg_segment_ptr());
   asm volatile("" : "+s"(at));
-  return *reinterpret_cast<const Args *>(at);
+  return *reinterpret_cast<const __attribute__((address_space(4))) Args *>(at);
 }
 
 __device__ __forceinline__ void report(uint32_t *status, uint32_t bits) {

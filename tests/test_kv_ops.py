@@ -644,3 +644,17 @@ def test_attend_refuses():
             B.make_rows(x)
     with pytest.raises(ValueError):
         B.make_scales(torch.zeros(4, 4), torch.zeros(4, 8))
+
+
+# ---------------------------------------------------------------- together, with the calls that move blocks
+
+@gpu
+def test_example_decodes_over_a_restored_prefix():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "decode_after_restore.py")
+    spec = importlib.util.spec_from_file_location("decode_after_restore", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    a, b = example.run(prompts=(200, 33, 16), chunk=96, steps=18)
+    assert a.shape == (18, 3, example.HQ, example.D) and torch.isfinite(a.float()).all() and torch.equal(a, b)
