@@ -243,6 +243,7 @@ int tutti_kv_append(const tutti_pool *pool, const tutti_scales *scales, const tu
   if (!aligned(d_status, 4)) return TUTTI_EINVAL;
   if (!good_rows(k) || !good_rows(v)) return TUTTI_EINVAL;
   if (q && (!good_rows(q) || !good_rows(q_out) || n_q_heads == 0)) return TUTTI_EINVAL;
+  if (q && n_q_heads > 0xffffu) return TUTTI_ERANGE;
   AppendArgs a{};
   if (rope) {
     RopeView &r = a.rope;

@@ -262,7 +262,11 @@ __device__ __forceinline__ void set_word(typename Words<N>::type &w, int i, uint
 // the queries and keys 4g..4g+3 of each half tile, which is how O^T = V^T P^T takes P, so weights stay in the lane that
 // made them.  The contraction's order is free: a lane loads 16 consecutive bytes of a key's row, and the queries are laid out to
 // match.  Of the values, a lane takes DP/16 consecutive ones of its eight keys, and puts pairs of keys together by byte
-// permutations; so nothing passes through LDS and no wavefront waits for another until the end, where the four join.
+// permutations; so nothing passes through LDS and no wavefront waits for another until the end, where those of a head join.
+// Bound by memory: 2*e*head_dim bytes a key and KV head for 4*group*head_dim flops.  32K tokens of 8 heads x 128 (128 MiB) in 28 us of
+// its own, 4.8 TB/s; 128K tokens in e4m3 (256 MiB) 52 us, 5.2 TB/s; 64 sequences in e4m3 (751 MB) 142 us, 5.3 TB/s.  The same loads
+// with no arithmetic reach 5.8 TB/s (nontemporal; four heads side by side, see heads_abreast), a launch of them takes 4 us to begin
+// and end: records, table, scales and first keys are four trips to memory one after the other.
 template <typename T, bool E4M3, int DP, bool FULL, bool PAGED16, int RT>
 __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2) void k_kv_attend(const AttendArgs a) {
   constexpr int ROWS = RT * 16, N = DP / 16;
@@ -669,6 +673,11 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2)
 // address a lane loads.  S^T = K Q^T and O^T = V^T P^T with 32x32x16 matrix instructions: lane (r = l % 32, h = l / 32) holds row r of the queries
 // and keys 8i+4h..8i+4h+3 of each 32, and the weights go from one product to the other where they are; values are read
 // transposed, four keys of 16 values at a time.
+// Bound by what a compute unit's wavefronts can issue: 2,048 queries behind 30,000 e4m3 tokens, 1.04 TFLOP, in 1.16 ms = 0.9 PFLOP/s (a
+// large library product: 1.18), where a wavefront issues half of its time, waits to issue a quarter and for LDS or its neighbours a
+// quarter; the matrix units are busy 37 % of the time, LDS as much.  With all loads from one tile the time is the same.  16-bit
+// prompts of 8,001 tokens, 0.12 TFLOP: 0.16 ms.  32 rows a wavefront, two wavefronts a SIMD: 64 rows need all registers of one, and
+// nothing covers its waits (1.94 ms).
 constexpr uint32_t kWideTile = 64;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -1245,7 +1254,8 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
 }
 
 // ---- Joins the parts of sequences that were split: one workgroup (WAVES 4) or one wavefront (1) a row.  DP/4 threads take a
-// part, four values each; so many parts go abreast, and four times that many are under way at once.
+// part, four values each; so many parts go abreast, and four times that many are under way at once.  Bound by its trips to memory:
+// records and plan, maxima, sums; 4.4 us for 4 parts, 6.7 for 128.
 template <typename T, int DP, int ROWS, int WAVES>
 __global__ __launch_bounds__(256) void k_kv_join(const AttendArgs a) {
   constexpr uint32_t TP = DP / 4, ABREAST = WAVES * kLanes / TP, U = 4;
@@ -1255,115 +1265,116 @@ __global__ __launch_bounds__(256) void k_kv_join(const AttendArgs a) {
   if (lane < a.batch.n_seq) plan.lane_seq = load_seq(a.batch.seqs + lane);
   // items: rows of the sequences that are split
   for (uint32_t item = WAVES == 1 ? blockIdx.x * 4 + uniform(wave) : blockIdx.x;; item += gridDim.x * (WAVES == 1 ? 4 : 1)) {
-  uint32_t before = 0, slots = 0, units = 0;
-  bool found = false;
-  uint32_t row0 = 0, parts = 0, local = 0, first_slot = 0, units_upto_it = 0;
-  for (uint32_t base = 0; base < a.batch.n_seq && !found; base += kLanes) {
-    tutti_seq s{};
-    uint32_t n = 0, split = 0, p = 0, all = 0;
-    if (base + lane < a.batch.n_seq) {
-      s = record(a, plan, base, lane);
-      if (seq_ok(a.batch, s) && s.n_new) {
-        p = parts_of(a, plan, s);
-        all = row_tiles<ROWS>(a, s) * (a.kv_heads / a.abreast) * p;
-        if (p > 1) {
-          n = s.n_new * a.group * a.kv_heads;
-          split = row_tiles<ROWS>(a, s) * a.kv_heads * p;
+    uint32_t before = 0, slots = 0, units = 0;
+    bool found = false;
+    uint32_t row0 = 0, parts = 0, local = 0, first_slot = 0, units_upto_it = 0;
+    for (uint32_t base = 0; base < a.batch.n_seq && !found; base += kLanes) {
+      tutti_seq s{};
+      uint32_t n = 0, split = 0, p = 0, all = 0;
+      if (base + lane < a.batch.n_seq) {
+        s = record(a, plan, base, lane);
+        if (seq_ok(a.batch, s) && s.n_new) {
+          p = parts_of(a, plan, s);
+          all = row_tiles<ROWS>(a, s) * (a.kv_heads / a.abreast) * p;
+          if (p > 1) {
+            n = s.n_new * a.group * a.kv_heads;
+            split = row_tiles<ROWS>(a, s) * a.kv_heads * p;
+          }
         }
       }
+      const uint32_t upto = before + lane_prefix_sum(n), split_upto = slots + lane_prefix_sum(split);
+      const uint32_t units_upto = units + lane_prefix_sum(all);
+      const uint64_t behind = __ballot(n != 0 && upto > item);
+      if (behind) {
+        const uint32_t l = static_cast<uint32_t>(__builtin_ctzll(behind));
+        found = true;
+        local = item - (from_lane(upto, l) - from_lane(n, l));
+        row0 = from_lane(s.row0, l);
+        parts = from_lane(p, l);
+        first_slot = from_lane(split_upto, l) - from_lane(split, l);
+        units_upto_it = from_lane(units_upto, l);
+      }
+      before = from_lane(upto, kLanes - 1);
+      slots = from_lane(split_upto, kLanes - 1);
+      units = from_lane(units_upto, kLanes - 1);
     }
-    const uint32_t upto = before + lane_prefix_sum(n), split_upto = slots + lane_prefix_sum(split);
-    const uint32_t units_upto = units + lane_prefix_sum(all);
-    const uint64_t behind = __ballot(n != 0 && upto > item);
-    if (behind) {
-      const uint32_t l = static_cast<uint32_t>(__builtin_ctzll(behind));
-      found = true;
-      local = item - (from_lane(upto, l) - from_lane(n, l));
-      row0 = from_lane(s.row0, l);
-      parts = from_lane(p, l);
-      first_slot = from_lane(split_upto, l) - from_lane(split, l);
-      units_upto_it = from_lane(units_upto, l);
-    }
-    before = from_lane(upto, kLanes - 1);
-    slots = from_lane(split_upto, kLanes - 1);
-    units = from_lane(units_upto, kLanes - 1);
-  }
-  if (!found) return;
-  const uint32_t heads = a.group * a.kv_heads, i = local / heads, head = local - i * heads;
-  const uint32_t kv = head / a.group, row = i * a.group + head - kv * a.group;
-  const uint32_t slot = first_slot + (row / ROWS * a.kv_heads + kv) * parts;
-  // what the attention kernel did not do is not joined
-  if (slot + parts > a.max_parts || units_upto_it > a.max_units) continue;
-  const uint64_t at0 = static_cast<uint64_t>(slot) * ROWS + row % ROWS;
+    if (!found) return;
+    const uint32_t heads = a.group * a.kv_heads, i = local / heads, head = local - i * heads;
+    const uint32_t kv = head / a.group, row = i * a.group + head - kv * a.group;
+    const uint32_t slot = first_slot + (row / ROWS * a.kv_heads + kv) * parts;
+    // what the attention kernel did not do, a workgroup's heads together, is not joined
+    if (first_slot + (row / ROWS * a.kv_heads + (kv / a.abreast + 1) * a.abreast) * parts > a.max_parts || units_upto_it > a.max_units)
+      continue;
+    const uint64_t at0 = static_cast<uint64_t>(slot) * ROWS + row % ROWS;
 
-  float top = kLowest;
-  for (uint32_t p = thread; p < parts; p += WAVES * kLanes) top = fmaxf(top, a.part_ml[at0 + static_cast<uint64_t>(p) * ROWS][0]);
+    float top = kLowest;
+    for (uint32_t p = thread; p < parts; p += WAVES * kLanes) top = fmaxf(top, a.part_ml[at0 + static_cast<uint64_t>(p) * ROWS][0]);
 #pragma unroll
-  for (int x = 1; x < 16; x <<= 1) top = fmaxf(top, __shfl_xor(top, x, kLanes));
-  top = max_over_rows(top);
-  __shared__ float tops[4], sums[4 * kLanes / TP];
-  __shared__ __attribute__((aligned(16))) float half[4 * kLanes / TP][DP];
-  if constexpr (WAVES != 1) {
-    if (lane == 0) tops[wave] = top;
-    __syncthreads();
+    for (int x = 1; x < 16; x <<= 1) top = fmaxf(top, __shfl_xor(top, x, kLanes));
+    top = max_over_rows(top);
+    __shared__ float tops[4], sums[4 * kLanes / TP];
+    __shared__ __attribute__((aligned(16))) float half[4 * kLanes / TP][DP];
+    if constexpr (WAVES != 1) {
+      if (lane == 0) tops[wave] = top;
+      __syncthreads();
 #pragma unroll
-    for (int x = 0; x < WAVES; ++x) top = fmaxf(top, tops[x]);
-  }
-  const uint32_t e = thread % TP * 4, mine = thread / TP;
-  float sum = 0.0f;
-  f32x4 y = {0, 0, 0, 0};
-  if (e < a.d) {
-    for (uint32_t p0 = mine; p0 < parts; p0 += U * ABREAST) {
-      f32x2 ml[U];
-      f32x4 o[U];
-#pragma unroll
-      for (uint32_t u = 0; u < U; ++u)
-        if (p0 + u * ABREAST < parts) {
-          const uint64_t at = at0 + static_cast<uint64_t>(p0 + u * ABREAST) * ROWS;
-          ml[u] = a.part_ml[at];
-          o[u] = *reinterpret_cast<const f32x4 *>(a.part_o + at * DP + e);
-        }
-#pragma unroll
-      for (uint32_t u = 0; u < U; ++u)
-        if (p0 + u * ABREAST < parts) {
-          const float by = __builtin_amdgcn_exp2f(ml[u][0] - top);
-          sum += by * ml[u][1];
-          y += by * o[u];
-        }
+      for (int x = 0; x < WAVES; ++x) top = fmaxf(top, tops[x]);
     }
-  }
-  // the parts that went abreast: in LDS, a wavefront in its own rows of it
-  const uint32_t first = WAVES == 1 ? uniform(wave) * ABREAST : 0;
-  *reinterpret_cast<f32x4 *>(&half[first + mine][e]) = y;
-  if (e == 0) sums[first + mine] = sum;
-  if constexpr (WAVES != 1) {
-    __syncthreads();
-  } else {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-  }
-  if (thread * 2 < a.d) {
-  float total = 0.0f;
-  f32x2 z = {0, 0};
+    const uint32_t e = thread % TP * 4, mine = thread / TP;
+    float sum = 0.0f;
+    f32x4 y = {0, 0, 0, 0};
+    if (e < a.d) {
+      for (uint32_t p0 = mine; p0 < parts; p0 += U * ABREAST) {
+        f32x2 ml[U];
+        f32x4 o[U];
 #pragma unroll
-  for (uint32_t w = 0; w < ABREAST; ++w) {
-    total += sums[first + w];
-    z += *reinterpret_cast<const f32x2 *>(&half[first + w][2 * thread]);
-  }
-  const float by = total > 0.0f || total != total ? 1.0f / total : 0.0f;
-  uint8_t *to = static_cast<uint8_t *>(a.out.base) + static_cast<uint64_t>(row0 + i) * a.out.row_stride + head * a.out.head_stride;
-  reinterpret_cast<typename T::two *>(to)[thread] =
-      typename T::two{static_cast<typename T::one>(z[0] * by), static_cast<typename T::one>(z[1] * by)};
-  if (thread == 0 && a.lse)
-    a.lse[static_cast<uint64_t>(row0 + i) * heads + head] =
-        total == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(total)) * kLn2;
-  }
-  if constexpr (WAVES != 1) {
-    __syncthreads();  // LDS is the next row's
-  } else {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-  }
+        for (uint32_t u = 0; u < U; ++u)
+          if (p0 + u * ABREAST < parts) {
+            const uint64_t at = at0 + static_cast<uint64_t>(p0 + u * ABREAST) * ROWS;
+            ml[u] = a.part_ml[at];
+            o[u] = *reinterpret_cast<const f32x4 *>(a.part_o + at * DP + e);
+          }
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u)
+          if (p0 + u * ABREAST < parts) {
+            const float by = __builtin_amdgcn_exp2f(ml[u][0] - top);
+            sum += by * ml[u][1];
+            y += by * o[u];
+          }
+      }
+    }
+    // the parts that went abreast: in LDS, a wavefront in its own rows of it
+    const uint32_t first = WAVES == 1 ? uniform(wave) * ABREAST : 0;
+    *reinterpret_cast<f32x4 *>(&half[first + mine][e]) = y;
+    if (e == 0) sums[first + mine] = sum;
+    if constexpr (WAVES != 1) {
+      __syncthreads();
+    } else {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+    if (thread * 2 < a.d) {
+      float total = 0.0f;
+      f32x2 z = {0, 0};
+#pragma unroll
+      for (uint32_t w = 0; w < ABREAST; ++w) {
+        total += sums[first + w];
+        z += *reinterpret_cast<const f32x2 *>(&half[first + w][2 * thread]);
+      }
+      const float by = total > 0.0f || total != total ? 1.0f / total : 0.0f;
+      uint8_t *to = static_cast<uint8_t *>(a.out.base) + static_cast<uint64_t>(row0 + i) * a.out.row_stride + head * a.out.head_stride;
+      reinterpret_cast<typename T::two *>(to)[thread] =
+          typename T::two{static_cast<typename T::one>(z[0] * by), static_cast<typename T::one>(z[1] * by)};
+      if (thread == 0 && a.lse)
+        a.lse[static_cast<uint64_t>(row0 + i) * heads + head] =
+            total == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(total)) * kLn2;
+    }
+    if constexpr (WAVES != 1) {
+      __syncthreads();  // LDS is the next row's
+    } else {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
   }
 }
 

@@ -2037,5 +2037,4 @@ int tutti_abi_describe(uint32_t *out, uint32_t cap) {
 
 namespace tutti {
 int hip_failed(int hip_error) { return hip_fail(static_cast<hipError_t>(hip_error)); }
-int compute_units() { return cu_count(); }
 }  // namespace tutti

@@ -610,6 +610,7 @@ def test_append_refuses():
         assert _code(B.tutti_kv_append, *_append_args(**kw)) == B.EINVAL, kw
     assert _code(B.tutti_kv_append, *_append_args(batch=dict(n_seq=B.MAX_REQ + 1))) == B.ERANGE
     assert _code(B.tutti_kv_append, *_append_args(batch=dict(n_rows=1 << 31))) == B.ERANGE
+    assert _code(B.tutti_kv_append, *_append_args(heads=1 << 16)) == B.ERANGE
     assert _code(B.tutti_kv_append, *_append_args(rows=dict(q=None, q_out=None), heads=0)) == B.OK
     for none in range(3):
         args = list(_append_args())
