@@ -276,8 +276,8 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2)
   using P = std::conditional_t<E4M3, Fp16, T>;
   using VWords = typename Words<VW>::type;
   // fp16 results: a weight is the sum of two fp16 numbers, so that its own rounding does not add to that of the result.  Decoding of
-  // small sequences (heads of 64, 16-bit blocks): error against 64 bits 2.2e-4 with one number, 1.9e-4 with two, where rounding
-  // the result alone gives 1.9e-4; 11.0 and 11.1 us, within what two runs differ.
+  // small sequences (heads of 64, 16-bit blocks): error against 64 bits 2.2e-4 with one number, 1.9e-4 with two (a plain
+  // product in 32 bits, rounded once at the end: 1.9e-4); 11.0 and 11.1 us, within what two runs differ.
   constexpr bool TWO = __is_same(T, Fp16);
 
   const uint32_t lane = threadIdx.x & (kLanes - 1), wave = uniform(threadIdx.x / kLanes);
@@ -683,8 +683,8 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2)
 // address a lane loads.  S^T = K Q^T and O^T = V^T P^T with 32x32x16 matrix instructions: lane (r = l % 32, h = l / 32) holds row r of the queries
 // and keys 8i+4h..8i+4h+3 of each 32, and the weights go from one product to the other where they are; values are read
 // transposed, four keys of 16 values at a time.
-// Bound by what a compute unit's wavefronts can issue: 2,048 queries behind 30,000 e4m3 tokens, 1.04 TFLOP, in 1.16 ms = 0.9 PFLOP/s (a
-// large library product: 1.18), where a wavefront issues half of its time, waits to issue a quarter and for LDS or its neighbours a
+// Bound by what a compute unit's wavefronts can issue: 2,048 queries behind 30,000 e4m3 tokens, 1.04 TFLOP, in 1.16 to 1.20 ms,
+// 0.87 to 0.9 PFLOP/s (a large library product: 1.18), where a wavefront issues half of its time, waits to issue a quarter and for LDS or its neighbours a
 // quarter; the matrix units are busy 37 % of the time, LDS as much.  With all loads from one tile the time is the same.  16-bit
 // prompts of 8,001 tokens, 0.12 TFLOP: 0.16 ms.  32 rows a wavefront, two wavefronts a SIMD: 64 rows need all registers of one, and
 // nothing covers its waits (1.94 ms).
