@@ -988,6 +988,8 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
 
   // Before tile t is worked on its scores are there, its values and the next tile's keys are in LDS; while it is worked on the next
   // tile's values and the keys of the one after that come in.
+  // A plane is filled only behind a barrier that is behind the last read of it, in the first turn too: some wavefronts read the first
+  // tile's keys for its scores, others, whose rows see nothing of it, go straight on to that turn, which fills the same plane.
   if (t1 > t0) {
     if (PAGED16)
       look_up_16(t0);
@@ -1009,10 +1011,8 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
   }
   for (uint32_t tile = t0; tile < t1; ++tile) {
     const uint32_t key0 = tile * kWideTile, v_at = v_of(tile), k_at = k_of(tile + 1);
-    if (tile != t0) {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
     const bool more = tile + 1 < t1, more_keys = tile + 2 < t1;
     if (E4M3 && !PAGED16) {
       per_key[wave][0][lane] = now.f;
