@@ -27,7 +27,7 @@
 
 namespace {
 
-enum Kind : uint8_t { kPointer, kStruct, kOptional, kInt };  // kOptional: a record, or what a pointer may be (None: no record)
+enum Kind : uint8_t { kPointer, kStruct, kOptional, kInt };  // kOptional: a record or None
 constexpr size_t kMaxArgs = 24;
 constexpr int kRecords = 9, kRequired = 4;  // classes of records; the first ones are always given as such
 
@@ -163,9 +163,11 @@ bool read_words(const Call *c, PyObject *const *args, size_t n_pos, PyObject *kw
     } else if (e.kind[i] == kInt) {
       if (!PyLong_CheckExact(x)) return false;
       word[i] = PyLong_AsUnsignedLongLongMask(x);
-    } else if (e.kind[i] == kPointer || (e.kind[i] == kOptional && reinterpret_cast<PyObject *>(Py_TYPE(x)) != g_records[e.record[i]])) {
+    } else if (e.kind[i] == kPointer || (e.kind[i] == kOptional && !g_records[e.record[i]])) {
       if (!pointer_word(x, &word[i])) return false;
-    } else {
+    } else if (e.kind[i] == kOptional && x == Py_None) {
+      word[i] = 0;
+    } else {  // a record, and no other thing that has an address: the library reads what is there
       if (reinterpret_cast<PyObject *>(Py_TYPE(x)) != g_records[e.record[i]]) return false;
       if (PyObject_GetBuffer(x, &views->view[views->n], PyBUF_SIMPLE) != 0) {
         PyErr_Clear();
@@ -273,7 +275,7 @@ PyObject *bind(PyObject *, PyObject *args) {
 }
 
 // setup(records, tensor type, function: current device, function: its current stream's handle, function: error check).  Of the
-// records the first kRequired have to be named; a class that is not named is not recognised.
+// records the first kRequired have to be named; where a class is not named, its arguments are plain pointers.
 PyObject *setup(PyObject *, PyObject *args) {
   PyObject *r, *o[4];
   if (!PyArg_ParseTuple(args, "O!OOOO", &PyTuple_Type, &r, &o[0], &o[1], &o[2], &o[3])) return nullptr;
