@@ -672,7 +672,7 @@ typedef struct tutti_attn {
  * fp16 result is the sum of two fp16 numbers), and the result once to dtype.  Scales are positive and finite.
  * d_work: work_bytes >= tutti_kv_attend_work_bytes(...) bytes of device memory (16-byte aligned, contents garbage before and
  * after) in which long sequences' parts meet; calls that may overlap need their own.  The size depends on the pool's shape,
- * batch->n_rows, n_seq, max_new and attn alone, and 0 comes back for arguments that the call refuses. */
+ * batch->n_rows, n_seq, max_new and attn alone, and 0 comes back where the call refuses one of these. */
 uint64_t tutti_kv_attend_work_bytes(const tutti_pool *pool, const tutti_batch *batch, const tutti_attn *attn);
 int tutti_kv_attend(const tutti_pool *pool, const tutti_scales *scales, const tutti_batch *batch, const tutti_attn *attn,
                     const tutti_rows *q, const tutti_rows *out, float *d_lse, void *d_work, uint64_t work_bytes,

@@ -16,7 +16,8 @@ using namespace tutti;
 
 bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
-int check_pool(const tutti_pool *pool, const tutti_scales *scales, uint32_t dtype) {
+// What of a call's arguments goes by sizes and types alone: the pool's, a batch's.
+int check_shape(const tutti_pool *pool, uint32_t dtype) {
   if (!pool) return TUTTI_EINVAL;
   if (dtype != TUTTI_BF16 && dtype != TUTTI_FP16) return TUTTI_EINVAL;
   if (pool->elt_bytes != 1 && pool->elt_bytes != 2) return TUTTI_EINVAL;
@@ -27,6 +28,15 @@ int check_pool(const tutti_pool *pool, const tutti_scales *scales, uint32_t dtyp
   if (b > 0xffffffffull) return TUTTI_EINVAL;
   b *= pool->head_dim * pool->elt_bytes;  // (at most 256)
   if (b > 0xffffffffull || pool->block_stride < b || pool->block_stride % 16 != 0) return TUTTI_EINVAL;
+  return TUTTI_OK;
+}
+int check_counts(const tutti_batch *b) {
+  if (!b) return TUTTI_EINVAL;
+  return b->n_seq > TUTTI_MAX_REQ || b->n_rows >= 0x80000000u ? TUTTI_ERANGE : TUTTI_OK;
+}
+
+int check_pool(const tutti_pool *pool, const tutti_scales *scales, uint32_t dtype) {
+  if (const int rc = check_shape(pool, dtype)) return rc;
   if (!pool->k_base || !pool->v_base || !aligned(pool->k_base, 16) || !aligned(pool->v_base, 16)) return TUTTI_EINVAL;
   if ((pool->elt_bytes == 1) != (scales != nullptr)) return TUTTI_EINVAL;
   if (scales && (!scales->k || !scales->v || !aligned(scales->k, 4) || !aligned(scales->v, 4) ||
@@ -36,8 +46,7 @@ int check_pool(const tutti_pool *pool, const tutti_scales *scales, uint32_t dtyp
 }
 
 int check_batch(const tutti_batch *b) {
-  if (!b) return TUTTI_EINVAL;
-  if (b->n_seq > TUTTI_MAX_REQ || b->n_rows >= 0x80000000u) return TUTTI_ERANGE;
+  if (const int rc = check_counts(b)) return rc;
   if (b->n_seq == 0 || b->n_rows == 0 || b->max_new == 0) return TUTTI_OK;
   if (!b->d_seqs || !aligned(b->d_seqs, 16)) return TUTTI_EINVAL;
   if (b->table_len && (!b->d_block_table || !aligned(b->d_block_table, 4))) return TUTTI_EINVAL;
@@ -303,7 +312,7 @@ int tutti_kv_append(const tutti_pool *pool, const tutti_scales *scales, const tu
 
 uint64_t tutti_kv_attend_work_bytes(const tutti_pool *pool, const tutti_batch *batch, const tutti_attn *attn) {
   AttendSizes s;
-  if (!pool || !batch || pool->num_kv_heads == 0 || check_attn(pool, attn) != TUTTI_OK) return 0;
+  if (!attn || check_shape(pool, attn->dtype) != TUTTI_OK || check_counts(batch) != TUTTI_OK || check_attn(pool, attn) != TUTTI_OK) return 0;
   if (attend_sizes(pool, batch, attn, &s) != TUTTI_OK) return 0;
   return s.bytes;
 }

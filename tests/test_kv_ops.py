@@ -647,6 +647,29 @@ def test_attend_refuses():
         B.make_scales(torch.zeros(4, 4), torch.zeros(4, 8))
 
 
+def test_work_bytes_refuses_what_the_call_refuses():
+    """Shapes, types and counts; not what only the call is handed (addresses, scales)."""
+    def size(pool=(), batch=(), attn=()):
+        p, b = B.make_pool(0, 0, **dict(GOOD, **dict(pool))), B.make_batch(0, 1, 1, 0, 4, 1)
+        a = B.make_attn(4, B.BF16, 0.1)
+        for record, fields in ((b, batch), (a, attn)):
+            for name, x in dict(fields).items():
+                setattr(record, name, x)
+        return B.tutti_kv_attend_work_bytes(p, b, a)
+
+    assert size() > 0 and size(pool=dict(elt_bytes=1)) > 0
+    for bad in BAD_POOLS:
+        if bad != dict(elt_bytes=1):        # (without scales: the call's matter)
+            assert size(pool=bad) == 0, bad
+    for bad in (dict(n_seq=B.MAX_REQ + 1), dict(n_rows=1 << 31), dict(n_rows=(1 << 31) - 1)):
+        assert size(batch=bad) == 0, bad
+    for bad in (dict(dtype=0), dict(dtype=3), dict(n_q_heads=0), dict(n_q_heads=5), dict(sm_scale=math.inf), dict(causal=2),
+                dict(causal=0, window=5)):
+        assert size(attn=bad) == 0, bad
+    assert B.tutti_kv_attend_work_bytes(B.make_pool(0, 0, **GOOD), None, B.make_attn(4, B.BF16, 0.1)) == 0
+    assert B.tutti_kv_attend_work_bytes(B.make_pool(0, 0, **GOOD), B.make_batch(0, 1, 1, 0, 4, 1), None) == 0
+
+
 # ---------------------------------------------------------------- together, with the calls that move blocks
 
 @gpu
