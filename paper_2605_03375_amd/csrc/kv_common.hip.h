@@ -19,7 +19,8 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr uint32_t kLanes = 64;
-constexpr float kLowest = -1e38f;  // stands for "nothing seen yet" in running maxima: finite, so that differences stay numbers
+// Stands for "nothing seen yet" in running maxima: finite, so that differences stay numbers, and no score that is finite is below it.
+constexpr float kLowest = -__FLT_MAX__;
 
 struct Fp16 {
   using one = _Float16;
