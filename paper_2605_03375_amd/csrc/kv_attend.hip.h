@@ -791,6 +791,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
   }
   f32x16 o[DT];
   float m = kLowest, l = 0.0f;
+  bool large = false;  // some row's m is
 #pragma unroll
   for (int n = 0; n < DT; ++n)
 #pragma unroll
@@ -1083,24 +1084,47 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
           rc16[x] = __uint_as_float(from_lane(__float_as_uint(looked.rc), from));
         }
       // the largest of each 16 keys, then with their factors of all
-      float top = kLowest;
+      float top = -__builtin_inff();
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         float most = sc[x / 2][8 * (x & 1)];
 #pragma unroll
         for (int i = 1; i < 8; ++i) most = fmaxf(most, sc[x / 2][8 * (x & 1) + i]);
-        if constexpr (E4M3 && PAGED16) most = most * f16[x] + lg16[x];
+        if constexpr (E4M3 && PAGED16) most = __builtin_fmaf(most, f16[x], lg16[x]);
         top = fmaxf(top, most);
       }
       if (!E4M3) top *= factor;
       top = max_of_halves(top);
-      if (__ballot(top > m + kRaise)) {
+      // A weight is 2^(score*factor - m) with the product not rounded by itself, where m is one that was: from 2^12 on the difference, 2^-12
+      // and more, would count beside 1, and from 2^27 on overflow.  There the products are rounded first, and m taken off them exactly.
+      float times = factor, from_m = m;
+      if (large || __ballot(top > m + kRaise)) {
         const float raised = top > m + kRaise ? top : m;
         const float by = __builtin_amdgcn_exp2f(m - raised);
         m = raised;
         l *= by;
 #pragma unroll
         for (int n = 0; n < DT; ++n) o[n] *= by;
+        from_m = m;
+        if constexpr (!E4M3 || PAGED16) {
+          constexpr uint32_t kLarge = 0x45800000u, kEnd = 0x7f7fffffu;  // magnitudes of 2^12 and more, but not that of kLowest
+          large = __ballot((__float_as_uint(m) & 0x7fffffffu) - kLarge < kEnd - kLarge) != 0;
+          if (large) {
+#pragma clang fp contract(off)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const float s = sc[x / 2][8 * (x & 1) + i], product = E4M3 ? __builtin_fmaf(s, f16[x], lg16[x]) : s * factor;
+                sc[x / 2][8 * (x & 1) + i] = product - m;
+              }
+              f16[x] = 1.0f;
+              lg16[x] = 0.0f;
+            }
+            times = 1.0f;
+            from_m = 0.0f;
+          }
+        }
       }
       // this tile's weights, two at a time, between the products of the next one's scores (of what lies there, if there is none:
       // nobody asks for them)
@@ -1121,7 +1145,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
         }
         if (y >= 16 - VALUES_EARLY) v[y - (16 - VALUES_EARLY)] = values_of(v_at, y - (16 - VALUES_EARLY), 0);
         const int x = y / 4;
-        const float f = E4M3 ? (PAGED16 ? f16[x] : 1.0f) : factor, less = (E4M3 && PAGED16 ? lg16[x] : 0.0f) - m;
+        const float f = E4M3 ? (PAGED16 ? f16[x] : 1.0f) : times, less = (E4M3 && PAGED16 ? lg16[x] : 0.0f) - from_m;
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
           const int i = (2 * y + z) % 8;

@@ -42,3 +42,41 @@ def test_scores_far_below_zero(seqs, T, cache):
             slack = np.repeat(np.abs(v[:n]).astype(np.float64).mean(0), st.group, 0) * ((n / 8 + 64) * ref.F32 + 2.0 ** -20)
             assert (np.abs(out[row0 + i] - want) <= 1.01 * ref.UNIT[st.dtype] * np.abs(want) + slack).all(), i
             assert (np.abs(lse[row0 + i] + 2.0 ** 126) <= 2.0 ** (126 - 20)).all(), i
+
+
+@gpu
+@pytest.mark.parametrize("cache", ["16", "e4m3"])
+@pytest.mark.parametrize("T", [16, 24])
+@pytest.mark.parametrize("size", [16, 26, 30, 34, 60, 110])
+@pytest.mark.parametrize("seqs", STEPS, ids=by_name)
+def test_scores_of_any_size(seqs, size, T, cache):
+    """Products of whole numbers times 2^size, exact in 32 bits, by a factor that is not: all weight is with the largest, in equal shares,
+    whatever the rounding of the factor's product is beside 1."""
+    st = Step(seqs, T=T, cache="e4m3" if cache == "e4m3" else None)
+    rng = np.random.default_rng(size)
+    st.q = rng.integers(-2, 3, st.q.shape).astype(np.float32)
+    k = rng.integers(-2, 3, st.cpu.planes[0].shape).astype(np.float32)
+    q, products = st.q.astype(np.float64), k.astype(np.float64)
+    st.q = st.q * np.float32(2.0 ** (size - size // 2))
+    if cache == "e4m3":
+        st.cpu.planes[0], st.cpu.scales[0][:], st.cpu.scales[1][:] = ref.to_e4m3(k), 2.0 ** (size // 2), 1.0
+    else:
+        st.cpu.planes[0] = k * np.float32(2.0 ** (size // 2))
+    out, lse, status = run_attend(st.to_gpu(), sm_scale=1.0 / 3)
+    assert status == 0
+    scale = float(np.float32(1.0 / 3)) * 2.0 ** size
+    for (row0, n_new, n_held, off) in st.seqs:
+        places = np.arange(n_held)
+        blocks = st.table[off + places // T]
+        v, kk = st.cpu.planes[1][blocks, places % T], products[blocks, places % T]
+        if cache == "e4m3":
+            v = ref.E4M3[v]
+        for i in range(n_new):
+            for head in range(st.hq):
+                n = n_held - n_new + i + 1
+                s = kk[:n, head // st.group] @ q[row0 + i, head]
+                top = v[:n, head // st.group][s == s.max()].astype(np.float64)
+                want, size_of = top.mean(0), np.abs(top).mean(0)
+                slack = size_of * (1.01 * ref.UNIT[st.dtype] + (n / 8 + 64) * ref.F32 + 2.0 ** -20)
+                assert (np.abs(out[row0 + i, head] - want) <= slack).all(), (i, head)
+                assert abs(lse[row0 + i, head] - scale * s.max()) <= 2.0 ** -20 * abs(scale * s.max()) + 8, (i, head)
