@@ -9,9 +9,13 @@ namespace tutti {
 constexpr uint32_t kKeyTile = 32;    // keys that a wavefront takes at a time: two halves of 16
 constexpr uint32_t kMostWaves = 5;   // wavefronts of a workgroup at most
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-// A row's running maximum is raised only by steps of more than this (log2): until then its weights are at most 2^8, far from
-// the largest fp16 value, and nothing that has been summed has to be rescaled.
+// A row's running maximum is raised only by steps of more than this (log2): until then nothing that has been summed has to be rescaled.
 constexpr float kRaise = 8.0f;
+// What a row's weights are relative to is its maximum less this (log2).  Weights that become fp16 are 2^15 at most (the largest fp16 value
+// is just below 2^16), keep their 11 bits down to 2^-21 of the largest and are off by 2^-32 of it at most below: of what a million keys that
+// far down add up to no more than 2^-12 is lost.  (Relative to the maximum itself it would be 2^-25 a key and 2^-5.)
+template <typename P>
+constexpr float kBelow = __is_same(P, Fp16) ? 7.0f : 0.0f;
 
 struct AttendArgs {
   PoolView pool;
@@ -395,8 +399,8 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2)
 #pragma unroll
       for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i]);
       top = max_over_rows(top);
-      if (__ballot(top > m[t] + kRaise)) {
-        const float raised = top > m[t] + kRaise ? top : m[t];
+      if (__ballot(top > m[t] + (kRaise + kBelow<P>))) {
+        const float raised = top > m[t] + (kRaise + kBelow<P>) ? top - kBelow<P> : m[t];
         const float by = __builtin_amdgcn_exp2f(m[t] - raised);
         m[t] = raised;
         l[t] *= by;
@@ -1098,8 +1102,8 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
       // A weight is 2^(score*factor - m) with the product not rounded by itself, where m is one that was: from 2^12 on the difference, 2^-12
       // and more, would count beside 1, and from 2^27 on overflow.  There the products are rounded first, and m taken off them exactly.
       float times = factor, from_m = m;
-      if (large || __ballot(top > m + kRaise)) {
-        const float raised = top > m + kRaise ? top : m;
+      if (large || __ballot(top > m + (kRaise + kBelow<P>))) {
+        const float raised = top > m + (kRaise + kBelow<P>) ? top - kBelow<P> : m;
         const float by = __builtin_amdgcn_exp2f(m - raised);
         m = raised;
         l *= by;

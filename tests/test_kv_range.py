@@ -1,4 +1,6 @@
 """Attention at the ends of the types' ranges, on the GPU against 64 bits: scores, weights and values that are very large or very small."""
+import math
+
 import numpy as np
 import pytest
 
@@ -80,3 +82,44 @@ def test_scores_of_any_size(seqs, size, T, cache):
                 slack = size_of * (1.01 * ref.UNIT[st.dtype] + (n / 8 + 64) * ref.F32 + 2.0 ** -20)
                 assert (np.abs(out[row0 + i, head] - want) <= slack).all(), (i, head)
                 assert abs(lse[row0 + i, head] - scale * s.max()) <= 2.0 ** -20 * abs(scale * s.max()) + 8, (i, head)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,cache", [("bf16", None), ("fp16", None), ("bf16", "e4m3"), ("fp16", "e4m3")])
+@pytest.mark.parametrize("T", [16, 24])
+@pytest.mark.parametrize("above", [10, 20, 25.5, 30])
+@pytest.mark.parametrize("n_new,n_seq", [(1, 1), (40, 1), (1, 600)])
+def test_many_small_weights(n_new, n_seq, above, T, dtype, cache):
+    """One key whose weight is 2^above times that of each other one, and whose value is 0: what the others add up to is the result.  A
+    weight keeps its type's precision down to 2^-21 of the largest, and is off by 2^-32 of that at most below.  (600 sequences, of the same
+    blocks, are not split.)"""
+    st = Step([(n_new, 8000)], T=T, dtype=dtype, cache=cache, h=1, group=1)
+    if n_seq > 1:
+        st.seqs, st.rows = [(i, 1, 8000, 0) for i in range(n_seq)], n_seq
+        st.q, st.k, st.v = (np.zeros((n_seq, 1, st.d), np.float32) for _ in range(3))
+    sm_scale = above * math.log(2.0)
+    st.q[:] = 0
+    st.q[:, :, 0] = 1
+    k, v = st.cpu.planes
+    rng = np.random.default_rng(4)
+    codes = rng.uniform(0.5, 1.0, v.shape)
+    v[:], k[:] = (ref.to_e4m3(codes), 0) if cache else (ref.round16(codes, dtype), 0)
+    for s in st.cpu.scales:
+        s[:] = 1.0
+    first = st.table[0]
+    k[first, 3, 0, 0] = ref.to_e4m3(1.0) if cache else 1.0
+    v[first, 3] = 0
+    out, lse, status = run_attend(st.to_gpu(), sm_scale=sm_scale)
+    assert status == 0
+    places = np.arange(8000)
+    values = v[st.table[places // T], places % T, 0]
+    values = ref.E4M3[values] if cache else values.astype(np.float64)
+    u_w = ref.UNIT["fp16" if cache else dtype]
+    for i in range(st.rows):
+        n = 8000 - n_new + i + 1 if n_seq == 1 else 8000
+        w = 2.0 ** (above * (places[:n] == 3) - above)
+        want = w @ values[:n] / w.sum()
+        ds = (st.d + 8) * ref.F32 * sm_scale + 2.0 ** -21
+        slack = (1.01 * ref.UNIT[dtype] + u_w + 2 * ds + 2 * (n / 8 + 64) * ref.F32) * want + n * 2.0 ** -32 + 2.0 ** -25
+        assert (np.abs(out[i, 0] - want) <= slack).all(), (i, np.abs(out[i, 0] - want).max(), slack.min())
+        assert abs(lse[i, 0] - (sm_scale + math.log(w.sum()))) <= ds + (n / 8 + 64) * ref.F32 + 2.0 ** -18
