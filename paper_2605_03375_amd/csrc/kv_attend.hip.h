@@ -189,6 +189,15 @@ __device__ __forceinline__ f32x4 product(typename T::eight a, typename T::eight 
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
+// A result, rounded.  A mean of fp16 values is no larger than they are, but weights that were rounded put one beside 65504 where it would
+// become an infinity: it stays 65504.  (Infinities and NaN stay what they are, and so do means of e4m3 values: `mean16` is false.)
+template <typename T>
+__device__ __forceinline__ typename T::one rounded(float y, bool mean16) {
+  if constexpr (__is_same(T, Fp16))
+    if (mean16 && fabsf(y) < __builtin_inff()) y = __builtin_amdgcn_fmed3f(y, -65504.0f, 65504.0f);
+  return static_cast<typename T::one>(y);
+}
+
 // Eight e4m3 codes as 16-bit values (exact in both types).
 template <typename T>
 __device__ __forceinline__ typename T::eight widen(u32x2 w) {
@@ -669,7 +678,7 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2)
       const float by = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
       typename T::eight y16;
 #pragma unroll
-      for (uint32_t c = 0; c < EACH; ++c) y16[c] = static_cast<typename T::one>(y[c] * by);
+      for (uint32_t c = 0; c < EACH; ++c) y16[c] = rounded<T>(y[c] * by, !E4M3);
       *reinterpret_cast<u32x4 *>(static_cast<uint8_t *>(z.out.base) + static_cast<uint64_t>(s.row0 + i) * z.out.row_stride +
                                  head * z.out.head_stride + 2 * e) = __builtin_bit_cast(u32x4, y16);
       if (e == 0 && z.lse)
@@ -1268,8 +1277,8 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
         typename T::two two[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          two[x][0] = static_cast<typename T::one>(o[n][i + 2 * x] * by);
-          two[x][1] = static_cast<typename T::one>(o[n][i + 2 * x + 1] * by);
+          two[x][0] = rounded<T>(o[n][i + 2 * x] * by, !E4M3);
+          two[x][1] = rounded<T>(o[n][i + 2 * x + 1] * by, !E4M3);
         }
         *(TUTTI_LDS u32x2 *)(mine + r * OUT_BYTES + (32 * n + 2 * i + 4 * hf) * 2) =
             u32x2{__builtin_bit_cast(uint32_t, two[0]), __builtin_bit_cast(uint32_t, two[1])};
@@ -1402,7 +1411,7 @@ __global__ __launch_bounds__(256) void k_kv_join(const AttendArgs a) {
       const float by = total > 0.0f || total != total ? 1.0f / total : 0.0f;
       uint8_t *to = static_cast<uint8_t *>(a.out.base) + static_cast<uint64_t>(row0 + i) * a.out.row_stride + head * a.out.head_stride;
       reinterpret_cast<typename T::two *>(to)[thread] =
-          typename T::two{static_cast<typename T::one>(z[0] * by), static_cast<typename T::one>(z[1] * by)};
+          typename T::two{rounded<T>(z[0] * by, !a.pool.k_scale), rounded<T>(z[1] * by, !a.pool.k_scale)};
       if (thread == 0 && a.lse)
         a.lse[static_cast<uint64_t>(row0 + i) * heads + head] =
             total == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(total)) * kLn2;

@@ -123,3 +123,17 @@ def test_many_small_weights(n_new, n_seq, above, T, dtype, cache):
         slack = (1.01 * ref.UNIT[dtype] + u_w + 2 * ds + 2 * (n / 8 + 64) * ref.F32) * want + n * 2.0 ** -32 + 2.0 ** -25
         assert (np.abs(out[i, 0] - want) <= slack).all(), (i, np.abs(out[i, 0] - want).max(), slack.min())
         assert abs(lse[i, 0] - (sm_scale + math.log(w.sum()))) <= ds + (n / 8 + 64) * ref.F32 + 2.0 ** -18
+
+
+@gpu
+@pytest.mark.parametrize("T", [16, 24])
+@pytest.mark.parametrize("seqs", [[(1, 900)], [(30, 300)], [(200, 700)]], ids=by_name)
+def test_largest_values(seqs, T):
+    """Values that are all the largest of fp16: so is every result, and it does not overflow by the roundings of its weights."""
+    st = Step(seqs, T=T, dtype="fp16", spread=2.0)
+    st.cpu.planes[1][:] = 65504.0
+    st.cpu.planes[1][:, :, 1] = -65504.0
+    out, _, status = run_attend(st.to_gpu())
+    assert status == 0
+    want = np.where(np.arange(st.hq) < st.group, 65504.0, -65504.0)[None, :, None]
+    assert (np.abs(out - want) <= 65504.0 * (2 * ref.UNIT["fp16"] + (seqs[0][1] / 8 + 64) * ref.F32)).all()
