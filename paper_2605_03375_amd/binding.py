@@ -354,11 +354,15 @@ def make_batch(d_seqs, n_seq, max_new, d_block_table, table_len, n_rows):
     return b
 
 
+def _is_of(x, floating, size):
+    return x.is_floating_point() == floating and x.element_size() == size
+
+
 def make_rows(rows, row_stride=None, head_stride=None):
     """Rows of vectors: a tensor [rows, heads, head size] whose heads are contiguous, or a pointer and byte strides."""
     if row_stride is None:
-        if rows.dim() != 3 or (rows.shape[2] > 1 and rows.stride(2) != 1):
-            raise ValueError("rows: a tensor [rows, heads, head size] with contiguous heads")
+        if rows.dim() != 3 or (rows.shape[2] > 1 and rows.stride(2) != 1) or not _is_of(rows, True, 2):
+            raise ValueError("rows: a tensor [rows, heads, head size] of a 16-bit type with contiguous heads")
         size = rows.element_size()
         row_stride, head_stride = rows.stride(0) * size, rows.stride(1) * size
     r = tutti_rows(_p(rows), row_stride, head_stride)
@@ -369,7 +373,7 @@ def make_rows(rows, row_stride=None, head_stride=None):
 def make_scales(k, v, stride=None):
     """Scales of an 8-bit pool: two tensors [blocks, floats of a row] of 32-bit floats, or pointers and the floats of a row."""
     if stride is None:
-        if k.shape != v.shape or k.stride() != v.stride() or k.stride(1) != 1 or k.element_size() != 4:
+        if k.dim() != 2 or k.shape != v.shape or k.stride() != v.stride() or k.stride(1) != 1 or not all(_is_of(x, True, 4) for x in (k, v)):
             raise ValueError("scales: two tensors [blocks, KV heads or more] of 32-bit floats, alike")
         stride = k.stride(0)
     s = tutti_scales(_p(k), _p(v), stride)
@@ -379,13 +383,24 @@ def make_scales(k, v, stride=None):
 
 def make_rope(d_cos_sin, rot_dim, n_pos=None, d_pos=None, pos_stride=None, pairs=None, interleaved=False):
     """Rotation by positions: d_cos_sin [positions, rot_dim]; d_pos [axes, rows] with `pairs` pairs of each axis, or None: a
-    token's place in its sequence."""
+    token's place in its sequence.  Either may be a pointer, with n_pos and pos_stride."""
+    pairs = (rot_dim // 2,) if pairs is None else pairs
+    if hasattr(d_cos_sin, "data_ptr"):
+        n_pos = d_cos_sin.shape[0] if n_pos is None else n_pos
+        if not _is_of(d_cos_sin, True, 4) or not d_cos_sin.is_contiguous() or n_pos * rot_dim > d_cos_sin.numel() or \
+                (d_cos_sin.dim() == 2 and d_cos_sin.shape[1] != rot_dim):
+            raise ValueError("angles: a contiguous tensor [positions, rot_dim] of 32-bit floats")
+    if hasattr(d_pos, "data_ptr"):
+        axes = d_pos.unsqueeze(0) if d_pos.dim() == 1 else d_pos
+        if not _is_of(d_pos, False, 4) or axes.dim() != 2 or (axes.shape[1] > 1 and axes.stride(1) != 1) or len(pairs) > axes.shape[0]:
+            raise ValueError("positions: a tensor [axes, rows] of 32-bit integers, rows side by side, and pairs for its axes")
+        pos_stride = axes.stride(0) if pos_stride is None else pos_stride
+    if n_pos is None or (d_pos is not None and pos_stride is None):
+        raise ValueError("angles or positions by pointer: n_pos, pos_stride")
     r = tutti_rope()
     r.d_cos_sin, r.d_pos, r.rot_dim, r.interleaved = _p(d_cos_sin), _p(d_pos), rot_dim, 1 if interleaved else 0
-    r.n_pos = d_cos_sin.shape[0] if n_pos is None else n_pos
-    if d_pos is not None:
-        r.pos_stride = d_pos.stride(0) if pos_stride is None else pos_stride
-    for i, n in enumerate((rot_dim // 2,) if pairs is None else pairs):
+    r.n_pos, r.pos_stride = n_pos, pos_stride or 0
+    for i, n in enumerate(pairs):
         r.axis_pairs[i] = n
     r._keep = (d_cos_sin, d_pos)
     return r
