@@ -430,8 +430,18 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2)
   // O^T += V^T P^T of a tile
   const auto values = [&](VWords (&vw)[8], uint32_t key0, bool edge, auto &&c, const typename P::eight (&p)[RT],
                           const typename P::eight (&low)[RT]) {
-    bool odd = false;
-    if (edge) {
+    bool odd = false, look = edge;
+    if constexpr (TWO && !E4M3) {
+      // the second number of a weight may be 0 or negative: an infinity must not meet it in tiles that all rows see either
+      f16x2 none = {0, 0};
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int x = 0; x < VW; ++x)
+          none = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, word<VW>(vw[i], x)), f16x2{0, 0}, none);
+      look |= __ballot(none[0] != none[0] || none[1] != none[1]) != 0;
+    }
+    if (look) {
       asm volatile("" ::);
       // values of keys that no row sees are whatever lies there: nothing of them may reach a product, not even times 0.  An infinity
       // or NaN that some rows see and others do not stays out of the products too and is added to the rows that see it (its weight is

@@ -137,3 +137,32 @@ def test_largest_values(seqs, T):
     assert status == 0
     want = np.where(np.arange(st.hq) < st.group, 65504.0, -65504.0)[None, :, None]
     assert (np.abs(out - want) <= 65504.0 * (2 * ref.UNIT["fp16"] + (seqs[0][1] / 8 + 64) * ref.F32)).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("T", [16, 24])
+@pytest.mark.parametrize("n_new", [4, 60, 150])
+def test_infinite_values(n_new, T, dtype):
+    """Infinities of both signs and NaN, in tiles that all rows see and in tiles that some do: each column is what the values that a row
+    sees add up to."""
+    n_held, marks = n_new + 400, {}
+    for at in (5, 333, 400, 402):
+        marks[at] = [(1, math.inf), (2, -math.inf), (3, math.nan)]
+    marks[7], marks[401], marks[403] = [(4, math.inf)], [(4, -math.inf), (5, math.inf)], [(5, -math.inf), (6, -math.inf)]
+    st = Step([(n_new, n_held)], T=T, dtype=dtype, d=128)
+    for at, columns in marks.items():
+        for column, x in columns:
+            st.cpu.planes[1][st.table[at // T], at % T, 1, column] = x
+    out, lse, status = run_attend(st.to_gpu())
+    assert status == 0 and np.isfinite(lse).all()
+    for i in range(n_new):
+        want = np.zeros(st.d)
+        for at, columns in marks.items():
+            if at <= n_held - n_new + i:
+                for column, x in columns:
+                    with np.errstate(invalid="ignore"):
+                        want[column] += x
+        for head in range(st.hq):
+            got = np.where(np.isfinite(out[i, head]), 0.0, out[i, head])
+            assert np.array_equal(got, want if head // st.group == 1 else np.zeros(st.d), equal_nan=True), (i, head)
