@@ -577,7 +577,10 @@ int tutti_place_pairs(const int32_t *classes, uint32_t n, uint32_t n_pairs, uint
  * Types.  `dtype` is the type of queries, keys, values and outputs.  pool->elt_bytes == 2: the blocks hold that type, and
  * `scales` is NULL.  pool->elt_bytes == 1: the blocks hold e4m3 values (1 sign, 4 exponent, 3 mantissa bits, no infinities,
  * largest 448) and `scales` one 32-bit factor for each block, KV head and plane: a cached value is code * scale.
- * head_dim is a multiple of 16 and at most 128 (else TUTTI_EINVAL). */
+ * head_dim is a multiple of 16 and at most 128 (else TUTTI_EINVAL).
+ *
+ * TUTTI_ERANGE: more than TUTTI_MAX_REQ sequences, 2^31 rows or (attention) rows times query heads and more, work memory that is too
+ * small, rows for which a launch would need 2^32 threads (rows that no sequence has count too). */
 #define TUTTI_BF16 1u
 #define TUTTI_FP16 2u
 #define TUTTI_ST_BAD_POS 32u /* tutti_kv_append: a position that the table of angles does not have: token skipped */

@@ -84,6 +84,8 @@ BatchView view(const tutti_batch *b) {
   return BatchView{b->d_seqs, b->d_block_table, b->n_seq, b->max_new, b->table_len, b->n_rows};
 }
 
+constexpr uint64_t kMostThreads = 0xffffffffull;  // of a launch
+
 int launched() {
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? TUTTI_OK : hip_failed(e);
@@ -164,7 +166,7 @@ int attend_sizes(const tutti_pool *pool, const tutti_batch *b, const tutti_attn 
   // each, so that they are no more than a round, and their parts no more than two.
   const uint64_t tiles = static_cast<uint64_t>(b->n_rows) * group / s->rows + std::min(b->n_seq, b->n_rows);
   const uint64_t units = 2 * s->slots + tiles * (pool->num_kv_heads / s->abreast);
-  if (units >= 0x80000000ull || static_cast<uint64_t>(b->n_rows) * attn->n_q_heads >= 0x80000000ull) return TUTTI_ERANGE;
+  if (units * 64 * (s->rows < 128 ? s->abreast * s->key_waves : 4) > kMostThreads || static_cast<uint64_t>(b->n_rows) * attn->n_q_heads >= 0x80000000ull) return TUTTI_ERANGE;
   s->max_units = static_cast<uint32_t>(units);
   s->max_parts = 2 * s->slots * s->abreast;
   s->ml_bytes = static_cast<uint64_t>(s->max_parts) * s->rows * sizeof(f32x2);
@@ -299,7 +301,7 @@ int tutti_kv_append(const tutti_pool *pool, const tutti_scales *scales, const tu
   a.heads_a_job = 4;
   a.q_jobs = (a.q_heads + a.heads_a_job - 1) / a.heads_a_job;
   a.jobs = a.q_jobs + 2 * (e4m3 ? a.kv_heads : (a.kv_heads + a.heads_a_job - 1) / a.heads_a_job);
-  if (units * a.jobs >= 0x80000000ull) return TUTTI_ERANGE;
+  if ((units * a.jobs + 3) / 4 * 256 > kMostThreads) return TUTTI_ERANGE;
   a.max_units = static_cast<uint32_t>(units);
   const uint32_t grid = static_cast<uint32_t>((units * a.jobs + 3) / 4);
   const hipStream_t st = static_cast<hipStream_t>(stream);

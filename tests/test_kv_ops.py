@@ -670,6 +670,22 @@ def test_work_bytes_refuses_what_the_call_refuses():
     assert B.tutti_kv_attend_work_bytes(B.make_pool(0, 0, **GOOD), B.make_batch(0, 1, 1, 0, 4, 1), None) == 0
 
 
+def test_more_threads_than_a_launch_has():
+    """2^32 threads and more: refused as such, before anything is launched."""
+    big = dict(n_seq=1, max_new=2)
+    for rows, pool in (((1 << 29) - 1, {}), (1 << 30, {}), ((1 << 31) - 1, {}), (1 << 30, dict(elt_bytes=1))):
+        args = _append_args(batch=dict(big, n_rows=rows), pool=pool, scales=SCALES if pool else None)
+        assert _code(B.tutti_kv_append, *args) == B.ERANGE, rows
+    for max_new, heads, rows in ((1, 2, 1 << 29), (20, 2, 1 << 28), (64, 2, (1 << 30) - 1)):
+        pool, _, batch, _, q, out, *_ = _append_args(batch=dict(n_seq=1, max_new=max_new, n_rows=rows))
+        attn = B.make_attn(heads, B.BF16, 0.1)
+        threads = (rows * heads // 2 // (16 if max_new == 1 else 32 if max_new == 20 else 128) + 1) * (1 if max_new < 64 else 2) * 256
+        refused = threads >= 1 << 32
+        assert (B.tutti_kv_attend_work_bytes(pool, batch, attn) == 0) == refused, max_new
+        if refused:
+            assert _code(B.tutti_kv_attend, pool, None, batch, attn, q, out, 0, FAKE, 1 << 60) == B.ERANGE, max_new
+
+
 # ---------------------------------------------------------------- together, with the calls that move blocks
 
 @gpu
