@@ -301,6 +301,17 @@ def test_append_is_within_its_roundings_of_64_bits():
             assert (np.abs(got - exact) <= 1.01 * unit * np.abs(exact) + slack * 2 + floor).all()
 
 
+@gpu
+@pytest.mark.parametrize("cache", ["16", "e4m3"])
+@pytest.mark.parametrize("rot,interleaved", [(64, False), (64, True), (62, False), (62, True), (6, False), (48, False)])
+def test_append_in_place_by_every_kind_of_rotation(rot, interleaved, cache):
+    """q_out is q: partners that lie in other lanes' vectors are read before any of them is written."""
+    rope = dict(cos_sin=make_angles(100, rot), rot=rot, interleaved=interleaved, pos=None, pairs=None)
+    for seqs in ([(20, 50), (1, 1)], [(1, 9)] * 5, [(2, 3)]):
+        st = Step(seqs, h=2, group=4, cache="e4m3" if cache == "e4m3" else None, held_before=False)
+        assert check_append(st, rope, in_place=True) == 0
+
+
 # ---------------------------------------------------------------- attend
 
 def run_attend(st, *, causal=True, window=0, sm_scale=None, with_lse=True, work_fill=0xff):
