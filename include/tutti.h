@@ -672,8 +672,9 @@ typedef struct tutti_attn {
  * (BAD_BLOCK).  Slots that no query of the sequence sees may hold anything, NaN included.
  * Scores, maxima, sums and products are 32-bit; the weights e^(s_j - max), of e4m3 values times the value's scale, are rounded to the
  * 16-bit type that meets the values in the matrix instructions (fp16 for e4m3 values, else dtype; where max_new*g is at most 32, a
- * weight of an fp16 result is the sum of two fp16 numbers), and the result once to dtype.  Weights that become fp16 lose bits
- * below 2^-21 of the largest one (scale included) and are 0 below 2^-32 of it.  Scales are positive and finite.
+ * weight of a 16-bit value or an fp16 result is the sum of two such numbers), and the result once to dtype.  Weights that become fp16
+ * lose bits below 2^-21 of the largest one (scale included) and are 0 below 2^-32 of it.  Values that are not finite make the results
+ * that see them not finite.  Scales are positive and finite.
  * d_work: work_bytes >= tutti_kv_attend_work_bytes(...) bytes of device memory (16-byte aligned, contents garbage before and
  * after) in which long sequences' parts meet; calls that may overlap need their own.  The size depends on the pool's shape,
  * batch->n_rows, n_seq, max_new and attn alone, and 0 comes back where the call refuses one of these. */

@@ -288,10 +288,11 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2)
   constexpr uint32_t EB = E4M3 ? 1 : 2;
   using P = std::conditional_t<E4M3, Fp16, T>;
   using VWords = typename Words<VW>::type;
-  // fp16 results: a weight is the sum of two fp16 numbers, so that its own rounding does not add to that of the result.  Decoding of
-  // small sequences (heads of 64, 16-bit blocks): error against 64 bits 2.2e-4 with one number, 1.9e-4 with two (a plain
-  // product in 32 bits, rounded once at the end: 1.9e-4); 11.0 and 11.1 us, within what two runs differ.
-  constexpr bool TWO = __is_same(T, Fp16);
+  // A weight is the sum of two numbers of its type, so that its own rounding does not add to that of the result.  Error against 64 bits
+  // with one and with two: 512 tokens of heads of 64, fp16 2.2e-4 and 1.9e-4, bf16 1.85e-3 and 1.53e-3 (a plain product in 32 bits, rounded
+  // once at the end: 1.9e-4 and 1.5e-3), both 11 to 12 us; 32K tokens of bf16 1.63e-3 and 1.59e-3, 34.5 and 35.0 us.  A bf16 result of e4m3
+  // values, whose weights are fp16, has no need of it (1.67e-3 and 1.66e-3).
+  constexpr bool TWO = __is_same(T, Fp16) || !E4M3;
 
   const uint32_t lane = threadIdx.x & (kLanes - 1), wave = uniform(threadIdx.x / kLanes);
   const uint32_t r = lane & 15u, g = lane >> 4;
@@ -433,13 +434,19 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2)
     bool odd = false, look = edge;
     if constexpr (TWO && !E4M3) {
       // the second number of a weight may be 0 or negative: an infinity must not meet it in tiles that all rows see either
-      f16x2 none = {0, 0};
+      typename T::two none = {0, 0};  // fp16: times 0, in pairs
+      float nil = 0.0f;               // bf16: the same by a product of two pairs
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int x = 0; x < VW; ++x)
-          none = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, word<VW>(vw[i], x)), f16x2{0, 0}, none);
-      look |= __ballot(none[0] != none[0] || none[1] != none[1]) != 0;
+        for (int x = 0; x < VW; ++x) {
+          const typename T::two v = __builtin_bit_cast(typename T::two, word<VW>(vw[i], x));
+          if constexpr (__is_same(T, Fp16))
+            none = __builtin_elementwise_fma(v, typename T::two{0, 0}, none);
+          else
+            nil = __builtin_amdgcn_fdot2_f32_bf16(v, none, nil, false);
+        }
+      look |= __ballot(nil != nil || none[0] != none[0] || none[1] != none[1]) != 0;
     }
     if (look) {
       asm volatile("" ::);

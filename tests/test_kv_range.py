@@ -166,3 +166,33 @@ def test_infinite_values(n_new, T, dtype):
         for head in range(st.hq):
             got = np.where(np.isfinite(out[i, head]), 0.0, out[i, head])
             assert np.array_equal(got, want if head // st.group == 1 else np.zeros(st.d), equal_nan=True), (i, head)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,cache", [("bf16", None), ("fp16", None), ("fp16", "e4m3")])
+@pytest.mark.parametrize("seqs,T", [([(1, 512)], 16), ([(3, 300), (1, 77)], 16), ([(7, 90)], 24)], ids=str)
+def test_weights_of_few_queries_add_no_rounding(seqs, T, dtype, cache):
+    """Two numbers to a weight: what is left of its rounding is that of the second, and the result's own is all that shows."""
+    st = Step(seqs, T=T, dtype=dtype, cache=cache, spread=2.0)
+    out, _, status = run_attend(st.to_gpu())
+    assert status == 0
+    for (row0, n_new, n_held, off) in st.seqs:
+        places = np.arange(n_held)
+        blocks = st.table[off + places // T]
+        k, v = (p[blocks, places % T] for p in st.cpu.planes)
+        if cache:
+            k, v = (ref.E4M3[x] * s[blocks][:, :, None] for x, s in zip((k, v), st.cpu.scales))
+        k, v = k.astype(np.float64), v.astype(np.float64)
+        for i in range(n_new):
+            for head in range(st.hq):
+                n, kv = n_held - n_new + i + 1, head // st.group
+                q = st.q[row0 + i, head].astype(np.float64)
+                s = k[:n, kv] @ q / math.sqrt(st.d)
+                w = np.exp(s - s.max())
+                w /= w.sum()
+                want, mag = w @ v[:n, kv], w @ np.abs(v[:n, kv])
+                size = (np.abs(k[:n, kv]) @ np.abs(q)).max() / math.sqrt(st.d)
+                ds = (st.d + 8) * ref.F32 * size + 2 * ref.F32 * np.abs(s).max() + 2.0 ** -21
+                bound = (2.0 * ref.UNIT[dtype] ** 2 + 2 * ds + 2 * (n / 8 + 64) * ref.F32) * mag * 1.01 + \
+                    ref.UNIT[dtype] * np.abs(want) * 1.01 + 2.0 ** -25
+                assert (np.abs(out[row0 + i, head] - want) <= bound).all(), (i, head)
