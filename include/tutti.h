@@ -674,7 +674,8 @@ typedef struct tutti_attn {
  * 16-bit type that meets the values in the matrix instructions (fp16 for e4m3 values, else dtype; where max_new*g is at most 32, a
  * weight of a 16-bit value or an fp16 result is the sum of two such numbers), and the result once to dtype.  Weights that become fp16
  * lose bits below 2^-21 of the largest one (scale included) and are 0 below 2^-32 of it.  Values that are not finite make the results
- * that see them not finite.  Scales are positive and finite.
+ * that see them not finite.  Scales are positive and finite.  Repeated calls give the same bits; beside other sequences in the call
+ * a sequence's results may differ within these roundings (max_new and all lengths decide how it is computed).
  * d_work: work_bytes >= tutti_kv_attend_work_bytes(...) bytes of device memory (16-byte aligned, contents garbage before and
  * after) in which long sequences' parts meet; calls that may overlap need their own.  The size depends on the pool's shape,
  * batch->n_rows, n_seq, max_new and attn alone, and 0 comes back where the call refuses one of these. */

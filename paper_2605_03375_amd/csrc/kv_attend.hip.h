@@ -269,7 +269,9 @@ __device__ __forceinline__ void set_word(typename Words<N>::type &w, int i, uint
     w[i] = x;
 }
 
-// ---- Few or many queries, one workgroup of four wavefronts to a (row tile, KV head, part of the keys).
+// ---- Few queries: a workgroup takes 16 or 32 rows of queries (RT 1 or 2), which is all that a sequence has, a group of `abreast`
+// neighbouring KV heads and a part of the keys.  Its wavefronts, 3 to 5: `key_waves` for each of the heads, which take the part's tiles
+// in turn.
 //
 // Scores are computed transposed, S^T = K Q^T, with 16x16x32 matrix instructions: lane (r = l % 16, g = l / 16) holds row r of
 // the queries and keys 4g..4g+3 of each half tile, which is how O^T = V^T P^T takes P, so weights stay in the lane that
@@ -713,11 +715,14 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2)
 // address a lane loads.  S^T = K Q^T and O^T = V^T P^T with 32x32x16 matrix instructions: lane (r = l % 32, h = l / 32) holds row r of the queries
 // and keys 8i+4h..8i+4h+3 of each 32, and the weights go from one product to the other where they are; values are read
 // transposed, four keys of 16 values at a time.
-// Bound by what a compute unit's wavefronts can issue: 2,048 queries behind 30,000 e4m3 tokens, 1.04 TFLOP, in 1.16 to 1.20 ms,
-// 0.87 to 0.9 PFLOP/s (a large library product: 1.18), where a wavefront issues half of its time, waits to issue a quarter and for LDS or its neighbours a
-// quarter; the matrix units are busy 37 % of the time, LDS as much.  With all loads from one tile the time is the same.  16-bit
-// prompts of 8,001 tokens, 0.12 TFLOP: 0.16 ms.  32 rows a wavefront, two wavefronts a SIMD: 64 rows need all registers of one, and
-// nothing covers its waits (1.94 ms).
+// Bound by what a compute unit's wavefronts can issue: 2,048 queries behind 30,000 e4m3 tokens, 1.04 TFLOP, in 1.17 to 1.21 ms,
+// 0.86 to 0.89 PFLOP/s (a large library product: 1.18), where a wavefront issues half of its time, waits to issue a quarter and for LDS or
+// its neighbours a quarter; the matrix units are busy 38 % of the time, LDS as much.  With all loads from one tile the time is the same.
+// The same of bf16 blocks 1.10 ms.  Prompts of 8,001 tokens in bf16, 0.12 TFLOP: 0.175 ms.  32 rows a wavefront, two wavefronts a SIMD: 64
+// rows need all registers of one, and nothing covers its waits (1.94 ms).
+// A weight is one number of its type, unlike where queries are few: with two the prompts take 0.214 ms (error against 64 bits 1.6e-3, with
+// one 2.1e-3, the plain product's 1.6e-3), the chunk of e4m3 blocks 1.58 ms (no less error: its weights are fp16), the fp16 prompts
+// 0.220 after 0.182 (2.1e-4, 2.6e-4).
 constexpr uint32_t kWideTile = 64;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
