@@ -718,11 +718,11 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2)
 // Bound by what a compute unit's wavefronts can issue: 2,048 queries behind 30,000 e4m3 tokens, 1.04 TFLOP, in 1.17 to 1.21 ms,
 // 0.86 to 0.89 PFLOP/s (a large library product: 1.18), where a wavefront issues half of its time, waits to issue a quarter and for LDS or
 // its neighbours a quarter; the matrix units are busy 38 % of the time, LDS as much.  With all loads from one tile the time is the same.
-// The same of bf16 blocks 1.10 ms.  Prompts of 8,001 tokens in bf16, 0.12 TFLOP: 0.175 ms.  32 rows a wavefront, two wavefronts a SIMD: 64
+// The same of bf16 blocks 1.04 ms.  Prompts of 8,001 tokens in bf16, 0.12 TFLOP: 0.165 ms.  32 rows a wavefront, two wavefronts a SIMD: 64
 // rows need all registers of one, and nothing covers its waits (1.94 ms).
-// A weight is one number of its type, unlike where queries are few: with two the prompts take 0.214 ms (error against 64 bits 1.6e-3, with
-// one 2.1e-3, the plain product's 1.6e-3), the chunk of e4m3 blocks 1.58 ms (no less error: its weights are fp16), the fp16 prompts
-// 0.220 after 0.182 (2.1e-4, 2.6e-4).
+// A weight is one number of its type, unlike where queries are few.  With one and with two, on one machine: the prompts 0.176 and 0.214 ms
+// (error against 64 bits 2.1e-3 and 1.6e-3, the plain product's 1.6e-3), in fp16 0.182 and 0.220 (2.6e-4 and 2.1e-4), the chunk of e4m3
+// blocks 1.18 and 1.58 (1.67e-3 and 1.66e-3: its weights are fp16).
 constexpr uint32_t kWideTile = 64;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
