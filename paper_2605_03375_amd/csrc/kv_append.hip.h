@@ -365,7 +365,8 @@ __device__ __forceinline__ void append_e4m3(const AppendArgs &a, const tutti_seq
 // Bound by memory, and by the launch below a megabyte: one token of 40 heads x 128 3.3 to 4.1 us; 256 sequences' tokens to e4m3 blocks 6.3
 // us (2.2 a launch, then four trips: record, table, angles and values, scale); 8,191 tokens to e4m3 blocks (189 MB) 46 us, 4.1 TB/s;
 // 16,384 tokens with three axes to 16-bit blocks (411 MB) 82 us, 5.0 TB/s (a large copy: 5.1 to 6.15).  Each kind of rotation has
-// kernels of its own: the general one needs 156 registers, which in every kernel made the first two cases 6.9 and 40 us.
+// kernels of its own: the general one needs 156 registers, which in every kernel made the first two cases 6.9 and 40 us.  By kind, those
+// 16,384 tokens: halves 83 us, pairs 77; with heads of 80 (floor 42 us) halves 63, pairs 55, 40 of 80 values rotated (value by value) 189.
 //
 // One wavefront, one job.  A unit is some tokens of one sequence: for 16-bit pools as many as a wavefront has rows of lanes, for
 // e4m3 pools those that go to one block.  Its jobs: queries, `heads_a_job` heads each, then keys and values, 16-bit as the

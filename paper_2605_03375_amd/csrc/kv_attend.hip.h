@@ -68,7 +68,8 @@ __device__ __forceinline__ tutti_seq record(const AttendArgs &a, const Plan &p, 
 // A part has the tiles that make the parts fill the device's slots once or, where that goes up better, twice: with one part more than
 // slots the last one has them for itself (32 sequences, 516 parts for 512 slots: 56 us, 488 parts: 42).  What is weighed is rounds times
 // (tiles of a part + kUnitTiles, what a workgroup costs beside its tiles).  More than 64 sequences, or more row tiles than two
-// rounds have slots for: an even share of all tiles, which leaves most sequences whole.
+// rounds have slots for: an even share of all tiles, which leaves most sequences whole (750 MB of bf16 cache in 64 sequences 134 us, in 65
+// 164, in 256 166; of e4m3 147 in 64, 210 in 512, 357 in 2,048, whose records every workgroup reads).
 constexpr uint32_t kUnitTiles = 8;
 
 template <int ROWS>
