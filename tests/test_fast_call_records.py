@@ -65,7 +65,7 @@ def test_what_is_no_record_is_left_to_the_wrapper(call_of, name):
 
 
 def test_a_tensor_in_place_of_rows_is_an_error():
-    """By ctypes and, on a GPU machine, by the module alike."""
+    """By ctypes and, where there is a GPU, by the module alike."""
     pool = B.make_pool(0x10000, 0x10000, num_blocks=4, block_tokens=16, num_kv_heads=2, head_dim=64, elt_bytes=2)
     batch, rows, x = B.make_batch(0x10000, 0, 1, 0x10000, 4, 1), B.make_rows(0x10000, 1024, 128), torch.zeros(4, 2, 64)
     for bad in (x, 4096, pool):
