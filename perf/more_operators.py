@@ -6,7 +6,7 @@ blocks that are shared, copied, given back and moved together.
   fork     tutti_blocks_fork: sequences that go on from another's blocks: its table entries shared, the last block as a copy of
            one's own, and new blocks where a sequence grows.  d_uses counts the table entries that name a block.
   free     tutti_blocks_free: table entries, and the blocks that nobody else names, given back.
-  compact  tutti_blocks_compact: the blocks in use become the first ones of the pool; tables follow.
+  compact  tutti_blocks_compact: the blocks in use become the first ones of the pool, the last of them first; tables follow.
   copy     tutti_blocks_copy: one layer's keys and values (codes and scales) of the blocks that were copied or moved.
 
 `own` chooses between the plain form in elementary torch operations and the framework's calls.  Fork, free and compact change
@@ -497,7 +497,8 @@ def _compact_plain(st):
     n_used = used.sum()
     holes, _, _ = _listed_places(~used & (ids < n_used))
     mover = used & (ids >= n_used)
-    rank, n = _ranked(mover)
+    rank, n = _ranked(mover.flip(0))                   # the last block first
+    rank = rank.flip(0)
     to = torch.where(mover, holes[rank], ids)
     pairs = torch.full((st.blocks + 1, 2), NONE, dtype=torch.int32, device=DEV)
     pairs[rank] = torch.stack([ids, to], 1).int()
@@ -590,7 +591,7 @@ def _exact_table(st):
     else:
         n = sum(u > 0 for u in uses)
         holes = [b for b in range(n) if uses[b] == 0]
-        movers = [b for b in range(n, st.blocks) if uses[b] > 0]
+        movers = [b for b in range(st.blocks - 1, n - 1, -1) if uses[b] > 0]
         pairs = list(zip(movers, holes))
         to = dict(pairs)
         for a, b in pairs:
