@@ -684,6 +684,87 @@ int tutti_kv_attend(const tutti_pool *pool, const tutti_scales *scales, const tu
                     const tutti_rows *q, const tutti_rows *out, float *d_lse, void *d_work, uint64_t work_bytes,
                     uint32_t *d_status, void *stream);
 
+/* The same for sequences that outlive their cache: beside the window's keys every query sees the first n_sinks tokens of its
+ * sequence.  Query i, at place p, sees key j if j < n_held and j <= p and (j > p - window or j < n_sinks).  Blocks in which no query
+ * of the step sees a key are not looked up: their table entries may name anything (TUTTI_NO_BLOCK once tutti_blocks_free has given
+ * them back), and nothing is reported for them.  n_sinks = 0, or attn->window = 0 (all keys are seen): as tutti_kv_attend.
+ * Everything else, the size of the work memory included, is as there. */
+int tutti_kv_attend_sinks(const tutti_pool *pool, const tutti_scales *scales, const tutti_batch *batch, const tutti_attn *attn,
+                          uint32_t n_sinks, const tutti_rows *q, const tutti_rows *out, float *d_lse, void *d_work,
+                          uint64_t work_bytes, uint32_t *d_status, void *stream);
+
+/* ---- blocks that several sequences use, and their coming and going.  A pool's blocks are counted in d_uses (device memory, 16-byte
+ * aligned, num_blocks words, one array for all layers, whose tables are the same): how many table entries name a block.  A block
+ * with no uses is free.  The calls below keep the counts; a table entry that names no block is TUTTI_NO_BLOCK, which they skip (the
+ * calls above, where they need the block, report it as BAD_BLOCK).  They go by device memory alone, in a fixed number of launches: what a step shares, copies or gives back may
+ * be decided on the GPU, and the whole step captured in a graph.  Results are the same from call to call.
+ * Common to them: num_blocks below 2^31, max_entries below 2^31 and at most TUTTI_MAX_REQ records (else TUTTI_ERANGE); d_block_table of
+ * table_len entries.  Calls on the same counts or tables, and the copies of blocks that they name, go in stream order. */
+#define TUTTI_NO_BLOCK 0xffffffffu /* a table entry, or a pair, that names no block */
+#define TUTTI_ST_NO_FREE 64u   /* tutti_blocks_fork: fewer free blocks than asked for: the entry is TUTTI_NO_BLOCK */
+#define TUTTI_ST_BAD_USES 128u /* tutti_blocks_free: a block that has no uses was to be given back: its count stays 0 */
+
+/* Where a sequence goes on from another's blocks, or grows: table entries [dst_off, dst_off + n_shared + n_copied + n_new) <-
+ * n_shared blocks that it shares (entries from src_off on; a use more for each), n_copied blocks of its own into which those named by
+ * the next n_copied entries of the source are to be copied, and n_new blocks of its own.  32 bytes, device memory, 16-byte aligned. */
+typedef struct tutti_fork {
+  uint32_t src_off;  /* not used where n_shared and n_copied are 0 */
+  uint32_t dst_off;
+  uint32_t n_shared;
+  uint32_t n_copied;
+  uint32_t n_new;
+  uint32_t rsvd[3];  /* not used */
+} tutti_fork;
+typedef struct tutti_block_pair {
+  uint32_t src;
+  uint32_t dst;
+} tutti_block_pair;
+typedef struct tutti_block_range {
+  uint32_t table_off;
+  uint32_t n_entries;
+} tutti_block_range;
+
+/* Fork.  The copied and new blocks of all records, in order, are numbered; number k gets the free block with the k-th lowest id (free
+ * when the call begins), one use.  Entries of the source that name no block are shared or copied as TUTTI_NO_BLOCK (those >=
+ * num_blocks too, BAD_BLOCK), and their number's block stays free.  d_pairs[p] <- (source's block, its copy) for the p-th copied
+ * entry of all records, (TUTTI_NO_BLOCK, TUTTI_NO_BLOCK) where there is no copy to make; *d_n_pairs (may be NULL) <- how many.  The caller
+ * has them copied in every layer (tutti_blocks_copy) before the sequences go on.
+ * Skipped with BAD_EXTENT, nothing of theirs written or numbered: records with more than max_entries entries, and those whose
+ * entries lie beyond the table; where the n_copied of the records so far add up to more than max_pairs, that record and all later ones.
+ * No destination may overlap another record's destination or any source (to go on in place, fork into a second table and free
+ * the first).  d_work: 16-byte aligned, work_bytes >= tutti_blocks_fork_work_bytes(...) (0: sizes that the call refuses), contents
+ * garbage before and after; calls that may overlap need their own. */
+uint64_t tutti_blocks_fork_work_bytes(uint32_t num_blocks, uint32_t n_forks);
+int tutti_blocks_fork(uint32_t *d_uses, uint32_t num_blocks, uint32_t *d_block_table, uint32_t table_len, const tutti_fork *d_forks,
+                      uint32_t n_forks, uint32_t max_entries, tutti_block_pair *d_pairs, uint32_t *d_n_pairs, uint32_t max_pairs,
+                      void *d_work, uint64_t work_bytes, uint32_t *d_status, void *stream);
+
+/* Free: every entry of the ranges becomes TUTTI_NO_BLOCK, and the block that it named loses a use.  A sequence that has ended gives all
+ * of its entries back; one that attends over a window those whose tokens no query will see again: with tutti_kv_attend_sinks, n_held
+ * tokens held and at least one to come, entry n where n*T >= n_sinks and (n + 1)*T <= n_held + 1 - window.  An entry in two ranges is
+ * given back once.  Ranges with more than max_entries entries, or beyond the table, are skipped (BAD_EXTENT); ids >= num_blocks become
+ * TUTTI_NO_BLOCK too (BAD_BLOCK). */
+int tutti_blocks_free(uint32_t *d_uses, uint32_t num_blocks, uint32_t *d_block_table, uint32_t table_len,
+                      const tutti_block_range *d_ranges, uint32_t n_ranges, uint32_t max_entries, uint32_t *d_status, void *stream);
+
+/* Compact: with n blocks in use, the k-th used block from the pool's end moves to the k-th free block from its begin, as long as it
+ * lies at n or behind it: the used ones are then the first n.  d_pairs[k] <- (from, to), and their counts move; every table entry
+ * that names one follows, whoever it belongs to.  d_totals[0] <- moves, d_totals[1] <- n.  At most max_pairs moves are made (there
+ * are never more than num_blocks / 2).  The caller has the blocks copied in every layer (tutti_blocks_copy: no block is both a
+ * source and a destination) before anything uses the table.  Entries >= num_blocks stay (BAD_BLOCK, but for TUTTI_NO_BLOCK).
+ * d_work as for tutti_blocks_fork. */
+uint64_t tutti_blocks_compact_work_bytes(uint32_t num_blocks);
+int tutti_blocks_compact(uint32_t *d_uses, uint32_t num_blocks, uint32_t *d_block_table, uint32_t table_len,
+                         tutti_block_pair *d_pairs, uint32_t *d_totals, uint32_t max_pairs, void *d_work, uint64_t work_bytes,
+                         uint32_t *d_status, void *stream);
+
+/* Copy: for each pair one layer's block src (T*h*d*e bytes of either plane, and with `scales` the scales of its KV heads) to block
+ * dst.  Any element size whose block is a multiple of 16 bytes; scales may be NULL.  d_n_pairs (device, may be NULL: max_pairs): how
+ * many pairs there are, at most max_pairs.  Pairs of TUTTI_NO_BLOCK are skipped, other ids >= num_blocks too (BAD_BLOCK).  A block that is a
+ * destination is in no other pair. */
+int tutti_blocks_copy(const tutti_pool *pool, const tutti_scales *scales, const tutti_block_pair *d_pairs, const uint32_t *d_n_pairs,
+                      uint32_t max_pairs, uint32_t *d_status, void *stream);
+
 /* ---- housekeeping */
 const char *tutti_strerror(int code);
 int tutti_last_hip_error(void);     /* hipError_t of the last failed HIP call on this thread, 0 if none */

@@ -33,6 +33,8 @@ STREAM_SLOTS = 4096
 IOCB_SLOTS = 2048
 MAX_REQ = 2048
 ST_BAD_BLOCK, ST_STAGE_CAP, ST_SQE_CAP, ST_DUP_BLOCK, ST_BAD_EXTENT, ST_BAD_POS = 1, 2, 4, 8, 16, 32
+ST_NO_FREE, ST_BAD_USES = 64, 128
+NO_BLOCK = 0xffffffff   # a table entry, or a pair, that names no block (-1 in tensors of 32-bit integers)
 BF16, FP16 = 1, 2   # types of queries, keys, values and outputs
 
 # Declarations of the C records for decoding results on the host.
@@ -44,6 +46,11 @@ SQE_DTYPE = np.dtype({"names": ["opcode", "kind", "layer", "file_id", "file_off"
                       "formats": ["u1", "u1", "<u2", "<u4", "<u8", "<u8", "<u4", "<u4", "<u8", "<u4", "<u4",
                                   ("u1", (16,))],
                       "offsets": [0, 1, 2, 4, 8, 16, 24, 28, 32, 40, 44, 48], "itemsize": 64})
+
+FORK_DTYPE = np.dtype([("src_off", "<u4"), ("dst_off", "<u4"), ("n_shared", "<u4"), ("n_copied", "<u4"), ("n_new", "<u4"),
+                       ("rsvd", "<u4", (3,))])
+PAIR_DTYPE = np.dtype([("src", "<u4"), ("dst", "<u4")])
+RANGE_DTYPE = np.dtype([("table_off", "<u4"), ("n_entries", "<u4")])
 
 SGL_DTYPE = np.dtype({"names": ["addr", "len", "id"], "formats": ["<u8", "<u4", "<u4"], "offsets": [0, 8, 12],
                       "itemsize": 16})
@@ -61,7 +68,8 @@ EXPORTS = ["tutti_obj_layout", "tutti_obj_pack", "tutti_obj_unpack", "tutti_sqe_
            "tutti_complete_io", "tutti_wait_cqe_range", "tutti_place_work_bytes", "tutti_place_pair_times",
            "tutti_place_classify", "tutti_place_pairs", "tutti_retrieve_layer_chained",
            "tutti_store_layer_chained", "tutti_issue_io_chained", "tutti_kv_append", "tutti_kv_attend",
-           "tutti_kv_attend_work_bytes"]
+           "tutti_kv_attend_work_bytes", "tutti_kv_attend_sinks", "tutti_blocks_fork", "tutti_blocks_fork_work_bytes",
+           "tutti_blocks_free", "tutti_blocks_compact", "tutti_blocks_compact_work_bytes", "tutti_blocks_copy"]
 BENCH_EXPORTS = ["tutti_copy_baseline", "tutti_stream_baseline", "tutti_scatter_baseline", "tutti_set_tuning",
                  "tutti_set_nontemporal", "tutti_set_hnd_mode", "tutti_set_xcd_mapping",
                  "tutti_host_cost_of_restore"]   # include/tutti_bench.h
@@ -208,6 +216,14 @@ def _declare(L, bench):
     L.tutti_kv_attend.argtypes = [pp, psc, pb, C.POINTER(tutti_attn), prows, prows, vp, vp, u64, vp, vp]
     L.tutti_kv_attend_work_bytes.argtypes = [pp, pb, C.POINTER(tutti_attn)]
     L.tutti_kv_attend_work_bytes.restype = u64
+    L.tutti_kv_attend_sinks.argtypes = [pp, psc, pb, C.POINTER(tutti_attn), u32, prows, prows, vp, vp, u64, vp, vp]
+    L.tutti_blocks_fork.argtypes = [vp, u32, vp, u32, vp, u32, u32, vp, vp, u32, vp, u64, vp, vp]
+    L.tutti_blocks_fork_work_bytes.argtypes = [u32, u32]
+    L.tutti_blocks_free.argtypes = [vp, u32, vp, u32, vp, u32, u32, vp, vp]
+    L.tutti_blocks_compact.argtypes = [vp, u32, vp, u32, vp, vp, u32, vp, u64, vp, vp]
+    L.tutti_blocks_compact_work_bytes.argtypes = [u32]
+    L.tutti_blocks_fork_work_bytes.restype = L.tutti_blocks_compact_work_bytes.restype = u64
+    L.tutti_blocks_copy.argtypes = [pp, psc, vp, vp, u32, vp, vp]
     L.tutti_strerror.argtypes = [C.c_int]
     L.tutti_strerror.restype = C.c_char_p
     L.tutti_version.restype = u32
@@ -233,7 +249,8 @@ def _declare(L, bench):
     L.tutti_place_pairs.argtypes = [C.POINTER(C.c_int32), u32, u32, u32, C.POINTER(u32), C.POINTER(u32)]
     for name in EXPORTS:
         if name not in ("tutti_strerror", "tutti_version", "tutti_sq_free_count", "tutti_table_validate_work_bytes",
-                        "tutti_table_order_work_bytes", "tutti_place_work_bytes", "tutti_kv_attend_work_bytes"):
+                        "tutti_table_order_work_bytes", "tutti_place_work_bytes", "tutti_kv_attend_work_bytes",
+                        "tutti_blocks_fork_work_bytes", "tutti_blocks_compact_work_bytes"):
             getattr(L, name).restype = C.c_int
     if bench:
         L.tutti_copy_baseline.argtypes = [vp, vp, u64, u32, vp]
@@ -819,6 +836,49 @@ def tutti_kv_attend(pool, scales, batch, attn, q, out, d_lse, d_work, work_bytes
                                                            _stream(stream)))
 
 
+def tutti_kv_attend_sinks(pool, scales, batch, attn, n_sinks, q, out, d_lse, d_work, work_bytes, d_status=None, stream=None):
+    """tutti_kv_attend whose queries see the first n_sinks tokens of their sequences beside attn's window."""
+    return _check("tutti_kv_attend_sinks", lib().tutti_kv_attend_sinks(_ref(pool), _ref(scales), _ref(batch), _ref(attn), n_sinks,
+                                                                       _ref(q), _ref(out), _p(d_lse), _p(d_work), work_bytes,
+                                                                       _p(d_status), _stream(stream)))
+
+
+def tutti_blocks_fork_work_bytes(num_blocks, n_forks):
+    return lib().tutti_blocks_fork_work_bytes(num_blocks, n_forks)
+
+
+def tutti_blocks_fork(d_uses, num_blocks, d_block_table, table_len, d_forks, n_forks, max_entries, d_pairs, d_n_pairs, max_pairs,
+                      d_work, work_bytes, d_status=None, stream=None):
+    """Sequences that go on from others' blocks (shared, or copied into free ones) and grow: tables, counts, blocks to be copied."""
+    return _check("tutti_blocks_fork", lib().tutti_blocks_fork(_p(d_uses), num_blocks, _p(d_block_table), table_len, _p(d_forks),
+                                                               n_forks, max_entries, _p(d_pairs), _p(d_n_pairs), max_pairs,
+                                                               _p(d_work), work_bytes, _p(d_status), _stream(stream)))
+
+
+def tutti_blocks_free(d_uses, num_blocks, d_block_table, table_len, d_ranges, n_ranges, max_entries, d_status=None, stream=None):
+    """Table entries given back, and with them the blocks that nothing else names."""
+    return _check("tutti_blocks_free", lib().tutti_blocks_free(_p(d_uses), num_blocks, _p(d_block_table), table_len, _p(d_ranges),
+                                                               n_ranges, max_entries, _p(d_status), _stream(stream)))
+
+
+def tutti_blocks_compact_work_bytes(num_blocks):
+    return lib().tutti_blocks_compact_work_bytes(num_blocks)
+
+
+def tutti_blocks_compact(d_uses, num_blocks, d_block_table, table_len, d_pairs, d_totals, max_pairs, d_work, work_bytes,
+                         d_status=None, stream=None):
+    """The blocks in use become the first ones of the pool: tables, counts, blocks to be copied."""
+    return _check("tutti_blocks_compact", lib().tutti_blocks_compact(_p(d_uses), num_blocks, _p(d_block_table), table_len,
+                                                                     _p(d_pairs), _p(d_totals), max_pairs, _p(d_work), work_bytes,
+                                                                     _p(d_status), _stream(stream)))
+
+
+def tutti_blocks_copy(pool, scales, d_pairs, d_n_pairs, max_pairs, d_status=None, stream=None):
+    """One layer's blocks (and scales) from the first of each pair to the second."""
+    return _check("tutti_blocks_copy", lib().tutti_blocks_copy(_ref(pool), _ref(scales), _p(d_pairs), _p(d_n_pairs), max_pairs,
+                                                               _p(d_status), _stream(stream)))
+
+
 def tutti_host_cost_of_restore(pool, cfg, d_n_blocks, n_req, d_block_table, table_len, d_file_id, layer, d_stage,
                                stage_cap, stage_addr, sgl_id, d_extents, d_totals, d_sqe, sqe_cap, n_calls,
                                cu_budget=0, d_status=None, stream=None):
@@ -838,7 +898,8 @@ _FAST_NAMES = ["tutti_layer_restore", "tutti_layer_save", "tutti_obj_layout", "t
                "tutti_sqe_build", "tutti_iocb_fill_direct", "tutti_issue_io", "tutti_issue_io_chained",
                "tutti_retrieve_layer", "tutti_store_layer", "tutti_retrieve_layer_issue", "tutti_store_layer_issue",
                "tutti_retrieve_layer_chained", "tutti_store_layer_chained", "tutti_complete_io", "tutti_kv_append",
-               "tutti_kv_attend"]
+               "tutti_kv_attend", "tutti_kv_attend_sinks", "tutti_blocks_fork", "tutti_blocks_free", "tutti_blocks_compact",
+               "tutti_blocks_copy"]
 _RECORDS = (tutti_pool, tutti_objcfg, tutti_ring, tutti_filestore, tutti_batch, tutti_rows, tutti_scales, tutti_rope, tutti_attn)
 _fast_call = None
 

@@ -18,11 +18,16 @@ BENCH_LIB = os.path.join(HERE, "libtutti_bench.so")  # the same sources with the
 # Python callables of the per-layer entry points (host code only); the name says which Python it is for
 FAST_CALL = os.path.join(HERE, "_fast_call" + sysconfig.get_config_var("EXT_SUFFIX"))
 FAST_CALL_DEPS = [os.path.join(CSRC, "fast_call.cpp"), os.path.join(ROOT, "include", "tutti.h")]
-SOURCES = [os.path.join(CSRC, "tutti_api.hip"), os.path.join(CSRC, "tutti_host.cpp"), os.path.join(CSRC, "kv_api.hip")]
+SOURCES = [os.path.join(CSRC, "tutti_api.hip"), os.path.join(CSRC, "tutti_host.cpp"), os.path.join(CSRC, "kv_api.hip"),
+           os.path.join(CSRC, "blocks_api.hip")]
+# attention kernels: a source for each type of queries, pool and kind of window
+SOURCES += [os.path.join(CSRC, f"kv_attend_{q}{pool}{kind}.hip")
+            for q in ("bf16", "fp16") for pool in ("", "_e4m3") for kind in ("", "_sinks")]
 DEPS = SOURCES + [os.path.join(CSRC, "tutti_kernels.hip.h"), os.path.join(CSRC, "launch_rules.h"),
                   os.path.join(CSRC, "layer_call.h"), os.path.join(CSRC, "library_state.h"),
                   os.path.join(CSRC, "kv_common.hip.h"), os.path.join(CSRC, "kv_append.hip.h"),
-                  os.path.join(CSRC, "kv_attend.hip.h"),
+                  os.path.join(CSRC, "blocks.hip.h"), os.path.join(CSRC, "kv_attend.hip.h"), os.path.join(CSRC, "kv_attend_launch.h"),
+                  os.path.join(CSRC, "kv_attend_launch.hip.h"),
                   os.path.join(ROOT, "include", "tutti.h"),
                   os.path.join(ROOT, "include", "tutti_bench.h")]
 
@@ -32,6 +37,8 @@ HIPCC_FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     # a kernel's first arguments, up to 14 words, are in scalar registers when a wavefront starts
     "-mllvm", "-amdgpu-kernarg-preload-count=14",
+    # the sources side by side
+    f"-parallel-jobs={min(8, os.cpu_count() or 1)}",
 ]
 
 

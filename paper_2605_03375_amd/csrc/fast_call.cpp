@@ -91,6 +91,8 @@ const Entry kEntries[] = {
     ENTRY(tutti_retrieve_layer),         ENTRY(tutti_store_layer),          ENTRY(tutti_retrieve_layer_issue),
     ENTRY(tutti_store_layer_issue),      ENTRY(tutti_retrieve_layer_chained), ENTRY(tutti_store_layer_chained),
     ENTRY(tutti_complete_io),            ENTRY(tutti_kv_append),            ENTRY(tutti_kv_attend),
+    ENTRY(tutti_kv_attend_sinks),        ENTRY(tutti_blocks_fork),          ENTRY(tutti_blocks_free),
+    ENTRY(tutti_blocks_compact),         ENTRY(tutti_blocks_copy),
 };
 #undef ENTRY
 

@@ -6,7 +6,7 @@
 #include <cmath>
 
 #include "kv_append.hip.h"
-#include "kv_attend.hip.h"
+#include "kv_attend_launch.h"
 #include "library_state.h"
 #include "tutti.h"
 
@@ -182,65 +182,59 @@ int check_attn(const tutti_pool *pool, const tutti_attn *attn) {
   return TUTTI_OK;
 }
 
-template <typename T, bool E4M3, int DP, bool PAGED16, int RT>
-void launch_attend(const AttendArgs &a, hipStream_t stream) {
-  const dim3 grid(a.max_units), wg(64 * a.abreast * a.key_waves);
-  if (a.d == DP)
-    hipLaunchKernelGGL((k_kv_attend<T, E4M3, DP, true, PAGED16, RT>), grid, wg, 0, stream, a);
-  else
-    hipLaunchKernelGGL((k_kv_attend<T, E4M3, DP, false, PAGED16, RT>), grid, wg, 0, stream, a);
-}
-template <typename T, int DP, int ROWS>
-void launch_join(const AttendArgs &a, hipStream_t stream) {
-  // a sequence that is split has two parts or more to a row tile, so no more rows are to be joined than this
-  const uint32_t joins = std::min(a.batch.n_rows * a.kv_heads * a.group, a.max_parts / 2 * ROWS);
-  // A workgroup a row for few rows, which may have many parts (32 rows of 128 parts: one wavefront, part after part, 75 us, four
-  // wavefronts 6.7, 16 wavefronts 6.2, but 1,280 rows of some parts 7.5 and 21); else a wavefront a row (1,511 queries of 20 heads in
-  // two parts: 20 us, with workgroups 61), 8192 at a time (8,001 prompt tokens that are not split: 5 us, with a wavefront for each row
-  // that there might be 21).
-  if (joins <= 4096)
-    hipLaunchKernelGGL((k_kv_join<T, DP, ROWS, 4>), dim3(joins), dim3(256), 0, stream, a);
-  else
-    hipLaunchKernelGGL((k_kv_join<T, DP, ROWS, 1>), dim3(2048), dim3(256), 0, stream, a);
-}
-template <typename T, bool E4M3, bool PAGED16>
-void launch_wide(const AttendArgs &a, hipStream_t stream) {
-  const dim3 grid(a.max_units), wg(256);
-  if (a.d == 128)
-    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 128, true, PAGED16>), grid, wg, 0, stream, a);
-  else if (a.d == 112)
-    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 112, true, PAGED16>), grid, wg, 0, stream, a);
-  else if (a.d == 96)
-    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 96, true, PAGED16>), grid, wg, 0, stream, a);
-  else if (a.d == 80)
-    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 80, true, PAGED16>), grid, wg, 0, stream, a);
-  else if (a.d == 64)
-    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 64, true, PAGED16>), grid, wg, 0, stream, a);
-  else
-    hipLaunchKernelGGL((k_kv_attend_wide<T, E4M3, 64, false, PAGED16>), grid, wg, 0, stream, a);
-}
-template <typename T, bool E4M3, int DP>
-void launch_attend(const AttendArgs &a, uint32_t rows, hipStream_t stream) {
-  if (rows == 128) {
-    if (a.pool.block_tokens % 16 == 0)
-      launch_wide<T, E4M3, true>(a, stream);
-    else
-      launch_wide<T, E4M3, false>(a, stream);
-    launch_join<T, DP, 128>(a, stream);
-    return;
-  }
-  if (a.pool.block_tokens % 16 == 0)
-    rows == 16 ? launch_attend<T, E4M3, DP, true, 1>(a, stream) : launch_attend<T, E4M3, DP, true, 2>(a, stream);
-  else
-    rows == 16 ? launch_attend<T, E4M3, DP, false, 1>(a, stream) : launch_attend<T, E4M3, DP, false, 2>(a, stream);
-  rows == 16 ? launch_join<T, DP, 16>(a, stream) : launch_join<T, DP, 32>(a, stream);
-}
 template <typename T>
 void launch_attend(const AttendArgs &a, bool e4m3, uint32_t rows, hipStream_t stream) {
+  // kernels of their own where first keys stay visible beside a window: the others have no tiles to leap over
   if (e4m3)
-    a.d <= 64 ? launch_attend<T, true, 64>(a, rows, stream) : launch_attend<T, true, 128>(a, rows, stream);
+    a.sinks ? launch_attend<T, true, true>(a, rows, stream) : launch_attend<T, true, false>(a, rows, stream);
   else
-    a.d <= 64 ? launch_attend<T, false, 64>(a, rows, stream) : launch_attend<T, false, 128>(a, rows, stream);
+    a.sinks ? launch_attend<T, false, true>(a, rows, stream) : launch_attend<T, false, false>(a, rows, stream);
+}
+
+// Both calls of attention; n_sinks: of tutti_kv_attend_sinks.
+int attend(const tutti_pool *pool, const tutti_scales *scales, const tutti_batch *batch, const tutti_attn *attn, uint32_t n_sinks,
+           const tutti_rows *q, const tutti_rows *out, float *d_lse, void *d_work, uint64_t work_bytes, uint32_t *d_status,
+           void *stream) {
+  if (!attn) return TUTTI_EINVAL;
+  int rc = check_pool(pool, scales, attn->dtype);
+  if (rc) return rc;
+  if ((rc = check_batch(batch)) != TUTTI_OK) return rc;
+  if ((rc = check_attn(pool, attn)) != TUTTI_OK) return rc;
+  if (!good_rows(q) || !good_rows(out) || !aligned(d_lse, 4) || !aligned(d_status, 4)) return TUTTI_EINVAL;
+  AttendSizes s;
+  if ((rc = attend_sizes(pool, batch, attn, &s)) != TUTTI_OK) return rc;
+  if (nothing_to_do(batch)) return TUTTI_OK;
+  if (!d_work || !aligned(d_work, 16)) return TUTTI_EINVAL;
+  if (work_bytes < s.bytes) return TUTTI_ERANGE;
+  AttendArgs a{};
+  a.pool = view(pool, scales);
+  a.batch = view(batch);
+  a.q = *q;
+  a.out = *out;
+  a.lse = d_lse;
+  a.kv_heads = pool->num_kv_heads;
+  a.group = attn->n_q_heads / pool->num_kv_heads;
+  a.d = pool->head_dim;
+  a.scale_log2 = attn->sm_scale * kLog2e;
+  a.causal = attn->causal;
+  a.window = attn->window;
+  a.abreast = s.abreast;
+  a.key_waves = s.key_waves;
+  a.slots = s.slots;
+  a.min_tiles = s.min_tiles;
+  a.max_units = s.max_units;
+  a.max_parts = s.max_parts;
+  a.tiles_a_part = static_cast<uint32_t *>(d_work);
+  a.part_ml = reinterpret_cast<f32x2 *>(static_cast<uint8_t *>(d_work) + 16);
+  a.part_o = reinterpret_cast<float *>(static_cast<uint8_t *>(d_work) + 16 + s.ml_bytes);
+  a.status = d_status;
+  if (attn->window) a.sinks = std::min(n_sinks, 0x7fffffffu);  // (without a window every key stays visible)
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  if (attn->dtype == TUTTI_BF16)
+    launch_attend<Bf16>(a, scales != nullptr, s.rows, st);
+  else
+    launch_attend<Fp16>(a, scales != nullptr, s.rows, st);
+  return launched();
 }
 
 }  // namespace
@@ -324,45 +318,13 @@ uint64_t tutti_kv_attend_work_bytes(const tutti_pool *pool, const tutti_batch *b
 int tutti_kv_attend(const tutti_pool *pool, const tutti_scales *scales, const tutti_batch *batch, const tutti_attn *attn,
                     const tutti_rows *q, const tutti_rows *out, float *d_lse, void *d_work, uint64_t work_bytes,
                     uint32_t *d_status, void *stream) {
-  if (!attn) return TUTTI_EINVAL;
-  int rc = check_pool(pool, scales, attn->dtype);
-  if (rc) return rc;
-  if ((rc = check_batch(batch)) != TUTTI_OK) return rc;
-  if ((rc = check_attn(pool, attn)) != TUTTI_OK) return rc;
-  if (!good_rows(q) || !good_rows(out) || !aligned(d_lse, 4) || !aligned(d_status, 4)) return TUTTI_EINVAL;
-  AttendSizes s;
-  if ((rc = attend_sizes(pool, batch, attn, &s)) != TUTTI_OK) return rc;
-  if (nothing_to_do(batch)) return TUTTI_OK;
-  if (!d_work || !aligned(d_work, 16)) return TUTTI_EINVAL;
-  if (work_bytes < s.bytes) return TUTTI_ERANGE;
-  AttendArgs a{};
-  a.pool = view(pool, scales);
-  a.batch = view(batch);
-  a.q = *q;
-  a.out = *out;
-  a.lse = d_lse;
-  a.kv_heads = pool->num_kv_heads;
-  a.group = attn->n_q_heads / pool->num_kv_heads;
-  a.d = pool->head_dim;
-  a.scale_log2 = attn->sm_scale * kLog2e;
-  a.causal = attn->causal;
-  a.window = attn->window;
-  a.abreast = s.abreast;
-  a.key_waves = s.key_waves;
-  a.slots = s.slots;
-  a.min_tiles = s.min_tiles;
-  a.max_units = s.max_units;
-  a.max_parts = s.max_parts;
-  a.tiles_a_part = static_cast<uint32_t *>(d_work);
-  a.part_ml = reinterpret_cast<f32x2 *>(static_cast<uint8_t *>(d_work) + 16);
-  a.part_o = reinterpret_cast<float *>(static_cast<uint8_t *>(d_work) + 16 + s.ml_bytes);
-  a.status = d_status;
-  const hipStream_t st = static_cast<hipStream_t>(stream);
-  if (attn->dtype == TUTTI_BF16)
-    launch_attend<Bf16>(a, scales != nullptr, s.rows, st);
-  else
-    launch_attend<Fp16>(a, scales != nullptr, s.rows, st);
-  return launched();
+  return attend(pool, scales, batch, attn, 0, q, out, d_lse, d_work, work_bytes, d_status, stream);
+}
+
+int tutti_kv_attend_sinks(const tutti_pool *pool, const tutti_scales *scales, const tutti_batch *batch, const tutti_attn *attn,
+                          uint32_t n_sinks, const tutti_rows *q, const tutti_rows *out, float *d_lse, void *d_work,
+                          uint64_t work_bytes, uint32_t *d_status, void *stream) {
+  return attend(pool, scales, batch, attn, n_sinks, q, out, d_lse, d_work, work_bytes, d_status, stream);
 }
 
 }  // extern "C"

@@ -33,6 +33,7 @@ struct AttendArgs {
   float *part_o;                // [part][rows][dp]: sums of weighted values
   f32x2 *part_ml;               // [part][rows]: running maximum (log2) and sum of weights
   uint32_t *status;
+  uint32_t sinks;               // the first keys, which stay visible (kernels with SINKS)
 };
 
 // Rows of a sequence: new tokens times query heads of a KV head, in tiles of ROWS.
@@ -41,14 +42,29 @@ __device__ __forceinline__ uint32_t row_tiles(const AttendArgs &a, const tutti_s
   return (s.n_new * a.group + ROWS - 1) / ROWS;
 }
 
+// Tiles with first keys that stay visible, as far as they are in front of tile `from`.
+template <uint32_t TILE>
+__device__ __forceinline__ uint32_t sink_tiles(uint32_t sinks, uint32_t from) {
+  return min((sinks + TILE - 1) / TILE, from);
+}
+
 // Key tiles that a sequence's queries see, counted from the tile of the first one.
 __device__ __forceinline__ uint32_t first_key(const AttendArgs &a, const tutti_seq &s) {
   const uint32_t begin = s.n_held - s.n_new;
   return a.window && begin + 1 > a.window ? begin + 1 - a.window : 0;
 }
+template <bool SINKS>
 __device__ __forceinline__ uint32_t key_tiles(const AttendArgs &a, const tutti_seq &s) {
-  return (s.n_held + kKeyTile - 1) / kKeyTile - first_key(a, s) / kKeyTile;
+  const uint32_t n = (s.n_held + kKeyTile - 1) / kKeyTile - first_key(a, s) / kKeyTile;
+  return SINKS ? n + sink_tiles<kKeyTile>(a.sinks, first_key(a, s) / kKeyTile) : n;
 }
+
+// SINKS: a row tile's key tiles by number: those of the first keys, then those from the window's first one on.  (`skip`: between them.)
+template <bool SINKS>
+struct TileOf {
+  uint32_t sinks, skip;
+  __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return SINKS && n >= sinks ? n + skip : n; }
+};
 
 // How many tiles a part of the keys has.  Every workgroup works this out from the records, which costs less than a launch before it.
 struct Plan {
@@ -56,8 +72,9 @@ struct Plan {
   tutti_seq lane_seq;  // record `lane` of the first 64: read once
 };
 
+template <bool SINKS>
 __device__ __forceinline__ uint32_t parts_of(const AttendArgs &a, const Plan &p, const tutti_seq &s) {
-  const uint32_t n = (key_tiles(a, s) + p.tiles_a_part - 1) / p.tiles_a_part;
+  const uint32_t n = (key_tiles<SINKS>(a, s) + p.tiles_a_part - 1) / p.tiles_a_part;
   return n ? n : 1;
 }
 
@@ -72,7 +89,7 @@ __device__ __forceinline__ tutti_seq record(const AttendArgs &a, const Plan &p, 
 // 164, in 256 166; of e4m3 147 in 64, 210 in 512, 357 in 2,048, whose records every workgroup reads).
 constexpr uint32_t kUnitTiles = 8;
 
-template <int ROWS>
+template <int ROWS, bool SINKS>
 __device__ __forceinline__ Plan make_plan(const AttendArgs &a) {
   const uint32_t lane = threadIdx.x & (kLanes - 1), head_groups = a.kv_heads / a.abreast;
   Plan p{};
@@ -84,7 +101,7 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs &a) {
       const tutti_seq s = record(a, p, base, lane);
       if (seq_ok(a.batch, s) && s.n_new) {
         rows = row_tiles<ROWS>(a, s) * head_groups;
-        tiles = key_tiles(a, s);
+        tiles = key_tiles<SINKS>(a, s);
         work += static_cast<uint64_t>(rows) * tiles;
       }
     }
@@ -135,7 +152,7 @@ struct Unit {
   uint32_t part_slot;   // of its first head's first part in the work memory, where parts > 1; the next head's are behind those
 };
 
-template <int ROWS>
+template <int ROWS, bool SINKS>
 __device__ __forceinline__ Unit locate(const AttendArgs &a, const Plan &p, uint32_t unit, bool first) {
   const uint32_t lane = threadIdx.x & (kLanes - 1);
   Unit u{};
@@ -151,7 +168,7 @@ __device__ __forceinline__ Unit locate(const AttendArgs &a, const Plan &p, uint3
       bad |= !ok;
       if (ok && s.n_new) {
         tiles = row_tiles<ROWS>(a, s);
-        parts = parts_of(a, p, s);
+        parts = parts_of<SINKS>(a, p, s);
         n = tiles * (a.kv_heads / a.abreast) * parts;
         split = parts > 1 ? tiles * a.kv_heads * parts : 0;
       }
@@ -283,7 +300,7 @@ __device__ __forceinline__ void set_word(typename Words<N>::type &w, int i, uint
 // its own, 4.8 TB/s; 128K tokens in e4m3 (256 MiB) 52 us, 5.2 TB/s; 64 sequences in e4m3 (751 MB) 142 us, 5.3 TB/s.  The same loads
 // with no arithmetic reach 5.8 TB/s (nontemporal; four heads side by side, see heads_abreast), a launch of them takes 4 us to begin
 // and end: records, table, scales and first keys are four trips to memory one after the other.
-template <typename T, bool E4M3, int DP, bool FULL, bool PAGED16, int RT>
+template <typename T, bool E4M3, int DP, bool FULL, bool PAGED16, int RT, bool SINKS>
 __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2) void k_kv_attend(const AttendArgs a) {
   constexpr int ROWS = RT * 16, N = DP / 16;
   constexpr int KW = E4M3 ? DP / 64 : DP / 32;       // 16-byte loads of a key a lane does
@@ -301,9 +318,9 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2)
   const uint32_t r = lane & 15u, g = lane >> 4;
   const bool reporter = blockIdx.x == 0 && wave == 0;
   if (blockIdx.x >= a.max_units) return;
-  const Plan plan = make_plan<ROWS>(a);
+  const Plan plan = make_plan<ROWS, SINKS>(a);
   if (reporter && (threadIdx.x & (kLanes - 1)) == 0) *a.tiles_a_part = plan.tiles_a_part;
-  const Unit u = locate<ROWS>(a, plan, blockIdx.x, reporter);
+  const Unit u = locate<ROWS, SINKS>(a, plan, blockIdx.x, reporter);
   if (u.seq == a.batch.n_seq) return;
   if (u.parts > 1 && u.part_slot + a.abreast * u.parts > a.max_parts) {
     if (threadIdx.x == 0) report(a.status, TUTTI_ST_BAD_EXTENT);
@@ -313,7 +330,7 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2)
   const uint32_t begin = s.n_held - s.n_new, n_rows = s.n_new * a.group;
   const uint32_t kv_head = u.head + wave % a.abreast, turn = wave / a.abreast;
 
-  // the keys that this lane's rows see: [lo, hi)
+  // the keys that this lane's rows see: those below hi but for lo of them, the first ones or (SINKS) those from a.sinks on
   uint32_t lo[RT], hi[RT];
   const uint8_t *q_at[RT];
 #pragma unroll
@@ -323,6 +340,7 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2)
     const uint32_t place = begin + i;
     hi[t] = a.causal ? place + 1 : s.n_held;
     lo[t] = a.window && place + 1 > a.window ? place + 1 - a.window : 0;
+    if (SINKS) lo[t] = lo[t] > a.sinks ? lo[t] - a.sinks : 0;
     q_at[t] = static_cast<const uint8_t *>(a.q.base) + static_cast<uint64_t>(s.row0 + i) * a.q.row_stride + head * a.q.head_stride;
   }
   // those that any row of the tile sees, and those that all of them see
@@ -332,9 +350,15 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2)
   const uint32_t any_lo = uniform(a.window && place_a + 1 > a.window ? place_a + 1 - a.window : 0);
   const uint32_t all_lo = uniform(a.window && place_b + 1 > a.window ? place_b + 1 - a.window : 0);
   const uint32_t tile_lo = any_lo / kKeyTile, tile_hi = (any_hi + kKeyTile - 1) / kKeyTile;
-  const uint32_t tiles = tile_hi - tile_lo;
-  const uint32_t t0 = uniform(tile_lo + static_cast<uint32_t>(static_cast<uint64_t>(tiles) * u.part / u.parts));
-  const uint32_t t1 = uniform(tile_lo + static_cast<uint32_t>(static_cast<uint64_t>(tiles) * (u.part + 1) / u.parts));
+  const uint32_t in_front = SINKS ? sink_tiles<kKeyTile>(a.sinks, tile_lo) : 0, t_base = SINKS ? 0 : tile_lo;
+  const TileOf<SINKS> tile_of{in_front, tile_lo - in_front};
+  const uint32_t tiles = tile_hi - tile_lo + in_front;
+  const uint32_t t0 = uniform(t_base + static_cast<uint32_t>(static_cast<uint64_t>(tiles) * u.part / u.parts));
+  const uint32_t t1 = uniform(t_base + static_cast<uint32_t>(static_cast<uint64_t>(tiles) * (u.part + 1) / u.parts));
+  // whether a key is among the n that a window hides; n for the keys that no row sees; whether a window hides some of a tile
+  const auto hidden = [&](uint32_t key, uint32_t n) { return (SINKS ? key - a.sinks : key) < n; };
+  const uint32_t any_hides = uniform(!SINKS ? any_lo : any_lo > a.sinks ? any_lo - a.sinks : 0);
+  const auto cut = [&](uint32_t key0, uint32_t window_lo) { return key0 < window_lo && (!SINKS || key0 + kKeyTile > a.sinks); };
 
   // queries, in the order of the contraction that the keys' loads give
   typename T::eight q[RT][DP / 32];
@@ -405,7 +429,7 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const uint32_t key = key0 + 16 * h + 4 * g + i;
-            if (!c(h, i).ok || key < lo[t] || key >= hi[t]) x[4 * h + i] = -__builtin_inff();
+            if (!c(h, i).ok || hidden(key, lo[t]) || key >= hi[t]) x[4 * h + i] = -__builtin_inff();
           }
       }
       float top = x[0];
@@ -459,7 +483,7 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const uint32_t key = key0 + 16 * (i / 4) + 4 * g + i % 4;
-        if (!c(i / 4, i % 4).ok || key < any_lo || key >= any_hi) vw[i] = VWords{};
+        if (!c(i / 4, i % 4).ok || hidden(key, any_hides) || key >= any_hi) vw[i] = VWords{};
 #pragma unroll
         for (int x = 0; x < VW; ++x) {
           uint32_t w = word<VW>(vw[i], x);
@@ -493,8 +517,9 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2)
       }
     }
     if (odd) {
-      const uint32_t from = key0 > any_lo ? key0 : any_lo, to = key0 + kKeyTile < any_hi ? key0 + kKeyTile : any_hi;
+      const uint32_t from = SINKS || key0 > any_lo ? key0 : any_lo, to = key0 + kKeyTile < any_hi ? key0 + kKeyTile : any_hi;
       for (uint32_t key = from; key < to; ++key) {
+        if (SINKS && hidden(key, any_hides)) continue;
         const uint32_t n = block_of(a.pool, key);
         const uint64_t at = static_cast<uint64_t>(s.table_off) + n;
         const uint32_t id = at < a.batch.table_len ? a.batch.table[at] : ~0u;
@@ -510,7 +535,7 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2)
             if (fabsf(x) < __builtin_inff()) continue;
 #pragma unroll
             for (int t = 0; t < RT; ++t)
-              if (key >= lo[t] && key < hi[t]) o[t][e][i] += x;
+              if (!hidden(key, lo[t]) && key < hi[t]) o[t][e][i] += x;
           }
         }
       }
@@ -539,11 +564,11 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2)
     uint64_t oks = 0;
     const uint32_t mine = t1 > t0 + turn ? (t1 - t0 - turn + a.key_waves - 1) / a.key_waves : 0;  // tiles
     const auto look_up = [&](uint32_t c) {
-      const uint32_t tile = t0 + turn + (c + lane / 2) * a.key_waves, key = tile * kKeyTile + 16 * (lane & 1u);
+      const uint32_t tile = t0 + turn + (c + lane / 2) * a.key_waves, key = tile_of(tile) * kKeyTile + 16 * (lane & 1u);
       const uint32_t n = block_of(a.pool, key);
       const uint64_t at = static_cast<uint64_t>(s.table_off) + n;
       uint32_t id = 0;
-      key_l.ok = tile < t1 && key + 16 > any_lo && key < any_hi;
+      key_l.ok = tile < t1 && (key + 16 > any_lo || (SINKS && key < a.sinks)) && key < any_hi;
       if (key_l.ok) {
         if (at < a.batch.table_len) id = a.batch.table[at];
         key_l.ok = at < a.batch.table_len && id < a.pool.num_blocks;
@@ -593,9 +618,9 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2)
       ask_values();
     }
     for (uint32_t c = 0; c < mine; ++c) {
-      const uint32_t key0 = (t0 + turn + c * a.key_waves) * kKeyTile;
+      const uint32_t key0 = tile_of(t0 + turn + c * a.key_waves) * kKeyTile;
       const Key now[2] = {x.key[0], x.key[1]};
-      const bool edge = key0 < all_lo || key0 + kKeyTile > all_hi || !now[0].ok || !now[1].ok;
+      const bool edge = cut(key0, all_lo) || key0 + kKeyTile > all_hi || !now[0].ok || !now[1].ok;
       const auto at = [&](int h, int) -> const Key & { return now[h]; };
       scores(x.kw, sc);
       const bool more = c + 1 < mine;
@@ -606,11 +631,11 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2)
     }
   } else {
     for (uint32_t tile = t0 + turn; tile < t1; tile += a.key_waves) {
-      const uint32_t key0 = tile * kKeyTile;
+      const uint32_t key0 = tile_of(tile) * kKeyTile;
       u32x4 kw[2][KW];
       VWords vw[8];
       Key key[2][4];
-      bool edge = key0 < all_lo || key0 + kKeyTile > all_hi;
+      bool edge = cut(key0, all_lo) || key0 + kKeyTile > all_hi;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         // lane r looks up key r of the half; the others' come from it
@@ -618,7 +643,7 @@ __global__ __launch_bounds__(64 * kMostWaves, RT == 1 && (FULL || E4M3) ? 3 : 2)
         const uint32_t n = block_of(a.pool, k);
         const uint64_t at = static_cast<uint64_t>(s.table_off) + n;
         uint32_t id = 0;
-        bool ok = k >= any_lo && k < any_hi;
+        bool ok = !hidden(k, any_hides) && k < any_hi;
         if (ok) {
           if (at < a.batch.table_len) id = a.batch.table[at];
           ok = at < a.batch.table_len && id < a.pool.num_blocks;
@@ -764,7 +789,7 @@ __device__ __forceinline__ float sum_of_halves(float x) {
 }
 
 // D: values of a head that it is built for; FULL: a head has so many (else fewer than 64, and D is 64).
-template <typename T, bool E4M3, int D, bool FULL, bool PAGED16>
+template <typename T, bool E4M3, int D, bool FULL, bool PAGED16, bool SINKS>
 __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
   constexpr int DP = D <= 64 ? 64 : 128, ROWS = 128, STEPS = D / 16, DT = (D + 31) / 32;
   constexpr uint32_t UNITS = DP / 8, ROW_BYTES = DP * 2, PLANE = kWideTile * ROW_BYTES;
@@ -779,9 +804,9 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
   const uint32_t r = lane & 31u, hf = lane >> 5;
   const bool reporter = blockIdx.x == 0 && wave == 0;
   if (blockIdx.x >= a.max_units) return;
-  const Plan plan = make_plan<ROWS>(a);
+  const Plan plan = make_plan<ROWS, SINKS>(a);
   if (reporter && (threadIdx.x & (kLanes - 1)) == 0) *a.tiles_a_part = plan.tiles_a_part;
-  const Unit u = locate<ROWS>(a, plan, blockIdx.x, reporter);
+  const Unit u = locate<ROWS, SINKS>(a, plan, blockIdx.x, reporter);
   if (u.seq == a.batch.n_seq) return;
   if (u.parts > 1 && u.part_slot + u.parts > a.max_parts) {
     if (threadIdx.x == 0) report(a.status, TUTTI_ST_BAD_EXTENT);
@@ -802,9 +827,16 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
   const uint32_t w_place_a = has_rows ? begin + wave_a / a.group : 0, w_place_b = has_rows ? begin + (wave_b - 1) / a.group : 0;
   const uint32_t w_any_lo = uniform(low(w_place_a)), w_any_hi = has_rows ? uniform(high(w_place_b)) : 0;
   const uint32_t w_all_lo = uniform(low(w_place_b)), w_all_hi = uniform(high(w_place_a));
-  const uint32_t tile_lo = any_lo / kWideTile, tiles = (any_hi + kWideTile - 1) / kWideTile - tile_lo;
-  const uint32_t t0 = uniform(tile_lo + static_cast<uint32_t>(static_cast<uint64_t>(tiles) * u.part / u.parts));
-  const uint32_t t1 = uniform(tile_lo + static_cast<uint32_t>(static_cast<uint64_t>(tiles) * (u.part + 1) / u.parts));
+  const uint32_t tile_lo = any_lo / kWideTile, in_front = SINKS ? sink_tiles<kWideTile>(a.sinks, tile_lo) : 0, t_base = SINKS ? 0 : tile_lo;
+  const TileOf<SINKS> tile_of{in_front, tile_lo - in_front};
+  const uint32_t tiles = (any_hi + kWideTile - 1) / kWideTile - tile_lo + in_front;
+  const uint32_t t0 = uniform(t_base + static_cast<uint32_t>(static_cast<uint64_t>(tiles) * u.part / u.parts));
+  const uint32_t t1 = uniform(t_base + static_cast<uint32_t>(static_cast<uint64_t>(tiles) * (u.part + 1) / u.parts));
+  // whether a window hides keys of a tile; (SINKS) which of a tile's keys it does not hide for being first ones
+  const auto cut = [&](uint32_t key0, uint32_t window_lo) { return key0 < window_lo && (!SINKS || key0 + kWideTile > a.sinks); };
+  const auto first_ones = [&](uint32_t key0) {
+    return !SINKS || key0 >= a.sinks ? 0 : a.sinks - key0 < kWideTile ? ~(~0ull << (a.sinks - key0)) : ~0ull;
+  };
 
   uint32_t lo, hi;  // of the lane's row
   typename T::eight q[STEPS];
@@ -871,9 +903,10 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
   } looked{};
   const auto look_up_16 = [&](uint32_t tile0) {
     looked.tile = tile0;
-    const uint32_t key = tile0 * kWideTile + 16 * lane, n = block_of(a.pool, key);
+    const uint32_t key = SINKS ? tile_of(tile0 + lane / 4) * kWideTile + 16 * (lane & 3u) : tile0 * kWideTile + 16 * lane;
+    const uint32_t n = block_of(a.pool, key);
     const uint64_t at = static_cast<uint64_t>(s.table_off) + n;
-    bool ok = key < t1 * kWideTile && key + 16 > any_lo && key < any_hi;
+    bool ok = (SINKS ? tile0 + lane / 4 < t1 : key < t1 * kWideTile) && (key + 16 > any_lo || (SINKS && key < a.sinks)) && key < any_hi;
     uint32_t id = 0;
     const bool asked = ok;
     if (ok) {
@@ -944,25 +977,29 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
   uint32_t id_next = 0;
   bool ok_next = false;
   const auto look_up_1 = [&](uint32_t tile) {
-    const uint32_t key = tile * kWideTile + lane;
+    const uint32_t key = tile_of(tile) * kWideTile + lane;
     const uint64_t at = static_cast<uint64_t>(s.table_off) + block_of(a.pool, key);
-    ok_next = tile < t1 && key >= any_lo && key < any_hi;
+    ok_next = tile < t1 && (key >= any_lo || (SINKS && key < a.sinks)) && key < any_hi;
     id_next = 0;
     if (ok_next) id_next = at < a.batch.table_len ? a.batch.table[at] : ~0u;
   };
   const auto find = [&](uint32_t tile, Tile &t) {
     if constexpr (PAGED16) {
-      const uint32_t key0 = tile * kWideTile;
+      const uint32_t key0 = tile_of(tile) * kWideTile;
       if (tile - looked.tile >= 16) look_up_16(tile - 2);
       const uint32_t four = static_cast<uint32_t>(looked.oks >> ((tile - looked.tile) * 4));
       t.oks = 0;
 #pragma unroll
       for (int x = 0; x < 4; ++x)
         if (four >> x & 1u) t.oks |= 0xffffull << (16 * x);
-      if (key0 < any_lo) t.oks &= ~0ull << (any_lo - key0);
+      if (SINKS) {
+        if (key0 < any_lo) t.oks &= (any_lo - key0 < kWideTile ? ~0ull << (any_lo - key0) : 0) | first_ones(key0);
+      } else if (key0 < any_lo) {
+        t.oks &= ~0ull << (any_lo - key0);
+      }
       if (key0 + kWideTile > any_hi) t.oks &= ~(~0ull << (any_hi - key0));  // (key0 < any_hi)
     } else {
-      const uint32_t key = tile * kWideTile + lane;
+      const uint32_t key = tile_of(tile) * kWideTile + lane;
       const bool lost = ok_next && id_next >= a.pool.num_blocks;
       skipped |= __ballot(lost) != 0;
       ok_next = ok_next && !lost;
@@ -995,7 +1032,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
   const auto seen_of = [&](uint32_t key0) {
     const uint32_t from = lo > key0 ? min(lo - key0, kWideTile) : 0, to = hi > key0 ? min(hi - key0, kWideTile) : 0;
     uint64_t bits = now.oks;
-    bits &= from < 64 ? ~0ull << from : 0;
+    bits &= (from < 64 ? ~0ull << from : 0) | first_ones(key0);
     bits &= to < 64 ? ~(~0ull << to) : ~0ull;
     return bits >> (4 * hf);
   };
@@ -1007,8 +1044,9 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
   const auto k_of = [&](uint32_t tile) { return (tile - t0 & 1u) * PLANE; };
   const auto v_of = [&](uint32_t tile) { return (2 + (tile - t0 & 1u)) * PLANE; };
   // the tiles that some row of the wavefront sees
-  const uint32_t w_t0 = has_rows ? max(t0, w_any_lo / kWideTile) : t1;
-  const uint32_t w_t1 = has_rows ? min(t1, (w_any_hi + kWideTile - 1) / kWideTile) : 0;
+  const uint32_t w_t0 = has_rows ? max(t0, w_any_lo / kWideTile - (SINKS ? tile_of.skip : 0)) : t1;
+  const uint32_t w_t1 = has_rows ? min(t1, (w_any_hi + kWideTile - 1) / kWideTile - (SINKS ? tile_of.skip : 0)) : 0;
+  const auto sees = [&](uint32_t tile) { return (tile >= w_t0 || (SINKS && tile_of(tile) * kWideTile < a.sinks)) && tile < w_t1; };
 
   // reads of LDS that are under way before the product that takes the first of them: of keys, of values, and of those between the
   // products of the keys already (e4m3 has fewer registers left: the rows that come in are there too)
@@ -1045,11 +1083,11 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (w_t0 == t0 && w_t1 > t0) scores_alone(t0);
+    if (SINKS ? sees(t0) : w_t0 == t0 && w_t1 > t0) scores_alone(t0);
     __syncthreads();
   }
   for (uint32_t tile = t0; tile < t1; ++tile) {
-    const uint32_t key0 = tile * kWideTile, v_at = v_of(tile), k_at = k_of(tile + 1);
+    const uint32_t key0 = tile_of(tile) * kWideTile, v_at = v_of(tile), k_at = k_of(tile + 1);
     const bool more = tile + 1 < t1, more_keys = tile + 2 < t1;
     if (E4M3 && !PAGED16) {
       per_key[wave][0][lane] = now.f;
@@ -1061,7 +1099,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
       find(tile + 2, second);
       bring(a.pool.k, tile + 2, second, k_of(tile + 2), raw_k);
     }
-    const bool wg_edge = key0 < all_lo || key0 + kWideTile > all_hi || now.oks != ~0ull;
+    const bool wg_edge = cut(key0, all_lo) || key0 + kWideTile > all_hi || now.oks != ~0ull;
     bool odd = false;
     if (wg_edge) {
       // values of keys that no row sees are whatever lies there, and an infinity or NaN that some rows see must not meet the others'
@@ -1086,7 +1124,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
       __syncthreads();
       odd = not_finite[0] | not_finite[1] | not_finite[2] | not_finite[3];
     }
-    if (tile >= w_t0 && tile < w_t1) {
+    if (sees(tile)) {
       typename T::eight k[2 * STEPS];
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i) k[i] = key_of(k_at, i);
@@ -1101,7 +1139,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
             for (int x = 0; x < 4; ++x) sc[h][i + x] = sc[h][i + x] * f[x] + lg[x];
           }
       }
-      if (key0 < w_all_lo || key0 + kWideTile > w_all_hi || now.oks != ~0ull) {
+      if (cut(key0, w_all_lo) || key0 + kWideTile > w_all_hi || now.oks != ~0ull) {
         asm volatile("" ::);  // (a branch: most tiles are whole ones)
         const uint64_t seen = seen_of(key0);
 #pragma unroll
@@ -1212,7 +1250,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
       __builtin_amdgcn_s_setprio(0);
 #pragma unroll
       for (int h = 0; h < 2; ++h) sc[h] = following[h];
-    } else if (tile + 1 == w_t0 && more) {
+    } else if (more && (SINKS ? sees(tile + 1) : tile + 1 == w_t0)) {
       scores_alone(tile + 1);
     }
     if (odd) {
@@ -1224,7 +1262,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
       for (uint32_t x = threadIdx.x; x < PLANE / 16; x += 256) {
         const uint32_t row = x / UNITS, d0 = ((x % UNITS) ^ swap_of<UNITS>(row)) * 8, key = key0 + row;
         typename P::eight w = {};
-        if (d0 < d && key >= any_lo && key < any_hi) {
+        if (d0 < d && (key >= any_lo || (SINKS && key < a.sinks)) && key < any_hi) {
           const uint32_t n = block_of(a.pool, key);
           const uint64_t at = static_cast<uint64_t>(s.table_off) + n;
           const uint32_t id = at < a.batch.table_len ? a.batch.table[at] : ~0u;
@@ -1328,7 +1366,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_wide(const AttendArgs a) {
 // ---- Joins the parts of sequences that were split: one workgroup (WAVES 4) or one wavefront (1) a row.  DP/4 threads take a
 // part, four values each; so many parts go abreast, and four times that many are under way at once.  Bound by its trips to memory:
 // records and plan, maxima, sums; 4.4 us for 4 parts, 6.7 for 128.
-template <typename T, int DP, int ROWS, int WAVES>
+template <typename T, bool E4M3, int DP, int ROWS, int WAVES, bool SINKS>
 __global__ __launch_bounds__(256) void k_kv_join(const AttendArgs a) {
   constexpr uint32_t TP = DP / 4, ABREAST = WAVES * kLanes / TP, U = 4;
   const uint32_t lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
@@ -1346,7 +1384,7 @@ __global__ __launch_bounds__(256) void k_kv_join(const AttendArgs a) {
       if (base + lane < a.batch.n_seq) {
         s = record(a, plan, base, lane);
         if (seq_ok(a.batch, s) && s.n_new) {
-          p = parts_of(a, plan, s);
+          p = parts_of<SINKS>(a, plan, s);
           all = row_tiles<ROWS>(a, s) * (a.kv_heads / a.abreast) * p;
           if (p > 1) {
             n = s.n_new * a.group * a.kv_heads;
@@ -1436,7 +1474,7 @@ __global__ __launch_bounds__(256) void k_kv_join(const AttendArgs a) {
       const float by = total > 0.0f || total != total ? 1.0f / total : 0.0f;
       uint8_t *to = static_cast<uint8_t *>(a.out.base) + static_cast<uint64_t>(row0 + i) * a.out.row_stride + head * a.out.head_stride;
       reinterpret_cast<typename T::two *>(to)[thread] =
-          typename T::two{rounded<T>(z[0] * by, !a.pool.k_scale), rounded<T>(z[1] * by, !a.pool.k_scale)};
+          typename T::two{rounded<T>(z[0] * by, !E4M3), rounded<T>(z[1] * by, !E4M3)};
       if (thread == 0 && a.lse)
         a.lse[static_cast<uint64_t>(row0 + i) * heads + head] =
             total == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(total)) * kLn2;

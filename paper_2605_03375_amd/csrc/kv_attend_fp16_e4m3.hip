@@ -1,0 +1,4 @@
+// Attention kernels: fp16 queries, e4m3 blocks.
+#include "kv_attend_launch.hip.h"
+
+template void tutti::launch_attend<tutti::Fp16, true, false>(const tutti::AttendArgs &, uint32_t, hipStream_t);
