@@ -176,6 +176,14 @@ int attend_sizes(const tutti_pool *pool, const tutti_batch *b, const tutti_attn 
   return TUTTI_OK;
 }
 
+// Key tiles that a tile of `rows` rows sees at most: the windows of its places, which follow each other, wherever they begin, and the
+// first keys.
+uint32_t most_tiles(uint32_t rows, uint32_t group, uint32_t window, uint32_t sinks) {
+  const uint64_t places = (rows + group - 2) / group + 1, keys = window + places - 1;
+  const uint64_t n = (keys + kKeyTile - 2) / kKeyTile + 1 + (static_cast<uint64_t>(sinks) + kKeyTile - 1) / kKeyTile;
+  return static_cast<uint32_t>(std::min<uint64_t>(n, 0x7fffffffu));
+}
+
 int check_attn(const tutti_pool *pool, const tutti_attn *attn) {
   if (!attn || attn->n_q_heads == 0 || attn->n_q_heads % pool->num_kv_heads != 0) return TUTTI_EINVAL;
   if (!std::isfinite(attn->sm_scale) || attn->causal > 1 || (attn->window && !attn->causal)) return TUTTI_EINVAL;
@@ -228,7 +236,12 @@ int attend(const tutti_pool *pool, const tutti_scales *scales, const tutti_batch
   a.part_ml = reinterpret_cast<f32x2 *>(static_cast<uint8_t *>(d_work) + 16);
   a.part_o = reinterpret_cast<float *>(static_cast<uint8_t *>(d_work) + 16 + s.ml_bytes);
   a.status = d_status;
-  if (attn->window) a.sinks = std::min(n_sinks, 0x7fffffffu);  // (without a window every key stays visible)
+  if (attn->window && n_sinks) {  // (without a window every key stays visible)
+    a.sinks = std::min(n_sinks, 0x7fffffffu);
+    a.most_tiles = most_tiles(s.rows, a.group, attn->window, a.sinks);
+    a.whole_tiles = s.rows < 128 ? 6 + s.key_waves * 5 / 2 : 12;
+    if (a.most_tiles <= a.whole_tiles) a.min_tiles = a.most_tiles;
+  }
   const hipStream_t st = static_cast<hipStream_t>(stream);
   if (attn->dtype == TUTTI_BF16)
     launch_attend<Bf16>(a, scales != nullptr, s.rows, st);

@@ -33,7 +33,8 @@ struct AttendArgs {
   float *part_o;                // [part][rows][dp]: sums of weighted values
   f32x2 *part_ml;               // [part][rows]: running maximum (log2) and sum of weights
   uint32_t *status;
-  uint32_t sinks;               // the first keys, which stay visible (kernels with SINKS)
+  // Kernels with SINKS: the first keys, which stay visible; key tiles that a row tile sees at most; how many do not pay for a join
+  uint32_t sinks, most_tiles, whole_tiles;
 };
 
 // Rows of a sequence: new tokens times query heads of a KV head, in tiles of ROWS.
@@ -56,7 +57,9 @@ __device__ __forceinline__ uint32_t first_key(const AttendArgs &a, const tutti_s
 template <bool SINKS>
 __device__ __forceinline__ uint32_t key_tiles(const AttendArgs &a, const tutti_seq &s) {
   const uint32_t n = (s.n_held + kKeyTile - 1) / kKeyTile - first_key(a, s) / kKeyTile;
-  return SINKS ? n + sink_tiles<kKeyTile>(a.sinks, first_key(a, s) / kKeyTile) : n;
+  // (SINKS: a row tile's share of a long prompt is its window's.  1,500 queries and 11 that decode, a window of 1,001 keys, 5 heads: parts
+  // by the keys that all of the sequence's rows see 91 us, by those of a row tile 69)
+  return SINKS ? min(n + sink_tiles<kKeyTile>(a.sinks, first_key(a, s) / kKeyTile), a.most_tiles) : n;
 }
 
 // SINKS: a row tile's key tiles by number: those of the first keys, then those from the window's first one on.  (`skip`: between them.)
@@ -95,7 +98,7 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs &a) {
   Plan p{};
   if (lane < a.batch.n_seq) p.lane_seq = load_seq(a.batch.seqs + lane);
   uint64_t work = 0;
-  uint32_t rows = 0, tiles = 0;  // of the lane's last sequence
+  uint32_t rows = 0, tiles = 0, most = 0;  // of the lane's last sequence; of all
   for (uint32_t base = 0; base < a.batch.n_seq; base += kLanes) {
     if (base + lane < a.batch.n_seq) {
       const tutti_seq s = record(a, p, base, lane);
@@ -103,11 +106,23 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs &a) {
         rows = row_tiles<ROWS>(a, s) * head_groups;
         tiles = key_tiles<SINKS>(a, s);
         work += static_cast<uint64_t>(rows) * tiles;
+        if (SINKS) most = max(most, tiles);
       }
     }
   }
 #pragma unroll
   for (int m = 1; m < static_cast<int>(kLanes); m <<= 1) work += __shfl_xor(work, m, kLanes);
+  if constexpr (SINKS) {
+    // Row tiles stay whole where the longest one ends with the others, or little later than parts and their join would: half of the slots
+    // keep the device busy.  128 sequences of 8 heads, windows of 1,024 keys: whole 95 us, in parts 106; 40 new tokens each of 1 head:
+    // 47 and 85; but one sequence of 8 heads 68 and 24.
+#pragma unroll
+    for (int m = 1; m < static_cast<int>(kLanes); m <<= 1) most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), m, kLanes)));
+    if (most <= work / (a.slots / 2) + a.whole_tiles) {
+      p.tiles_a_part = uniform(most ? most : 1);
+      return p;
+    }
+  }
   const auto share = [&](uint32_t slots) {
     const uint64_t each = (work + slots - 1) / slots;
     const uint32_t most = 0x40000000u, n = each > most ? most : static_cast<uint32_t>(each);

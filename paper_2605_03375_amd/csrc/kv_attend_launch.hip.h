@@ -18,13 +18,15 @@ void launch_few(const AttendArgs &a, hipStream_t stream) {
 }
 template <typename T, bool E4M3, bool SINKS, int DP, int ROWS>
 void launch_join(const AttendArgs &a, hipStream_t stream) {
+  if (SINKS && a.most_tiles <= a.min_tiles) return;  // nothing is split
   // a sequence that is split has two parts or more to a row tile, so no more rows are to be joined than this
   const uint32_t joins = std::min(a.batch.n_rows * a.kv_heads * a.group, a.max_parts / 2 * ROWS);
   // A workgroup a row for few rows, which may have many parts (32 rows of 128 parts: one wavefront, part after part, 75 us, four
   // wavefronts 6.7, 16 wavefronts 6.2, but 1,280 rows of some parts 7.5 and 21); else a wavefront a row (1,511 queries of 20 heads in
   // two parts: 20 us, with workgroups 61), 8192 at a time (8,001 prompt tokens that are not split: 5 us, with a wavefront for each row
   // that there might be 21).
-  if (joins <= 4096)
+  // (SINKS, whose windows bound the parts of a row: 2,048 rows of four parts, workgroups 7.9 us, wavefronts 5.)
+  if (joins <= (SINKS && a.most_tiles <= 32 * a.min_tiles ? 1024 : 4096))
     hipLaunchKernelGGL((k_kv_join<T, E4M3, DP, ROWS, 4, SINKS>), dim3(joins), dim3(256), 0, stream, a);
   else
     hipLaunchKernelGGL((k_kv_join<T, E4M3, DP, ROWS, 1, SINKS>), dim3(2048), dim3(256), 0, stream, a);

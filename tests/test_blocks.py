@@ -43,7 +43,9 @@ class Pool:
         assert got[:16] == got[-16:] == [5] * 16 and got[16:-16] == self.table
         assert int(self.d_status.item()) == status
 
-    def fork(self, records, max_entries=None, max_pairs=None, work_fill=0xff, check=True):
+    def fork(self, records, max_entries=None, max_pairs=None, work_fill=0xff, pad=0):
+        """pad: so many records without entries behind these (over 1,024 records in all, two launches do what one does else)."""
+        records = records + [(0, 0, 0, 0, 0)] * pad
         if max_entries is None:
             max_entries = max([s + c + n for _, _, s, c, n in records] + [1])
         if max_pairs is None:
@@ -57,8 +59,6 @@ class Pool:
         work = torch.full((need + 16,), work_fill, dtype=torch.uint8, device=DEV)
         B.tutti_blocks_fork(self.d_uses, len(self.uses), self.d_table, len(self.table), d_rec, len(records), max_entries, pairs, n_pairs,
                             max_pairs, work, need, self.d_status)
-        if not check:
-            return
         want, status = ref.fork(self.uses, self.table, records, max_entries, max_pairs)
         self.check(status)
         assert back(n_pairs) == [len(want)]
@@ -111,13 +111,30 @@ def random_pool(blocks, n_seq, width, rng, share=0.5, halves=2):
 
 # ---------------------------------------------------------------- fork
 
+both = pytest.mark.parametrize("pad", [0, 1100])
+
+
 @gpu
-@pytest.mark.parametrize("blocks", [1, 2, 3, 4, 5, 1023, 1024, 1025, 4099, 70001])
-def test_new_blocks_are_the_lowest_free_ones(blocks):
+@pytest.mark.parametrize("blocks", [1, 2, 3, 4, 5, 1023, 1024, 1025, 4099, 16384, 16390, 65533, 65536, 65537, 70001])
+@pytest.mark.parametrize("most", [800, 1300])
+def test_new_blocks_are_the_lowest_free_ones(blocks, most):
+    """One launch (up to 65,536 blocks and 4,096 entries) and two."""
     rng = random.Random(blocks)
-    for free_share in (0.0, 0.02, 0.5, 1.0):
+    for free_share in (0.0, 0.003, 0.02, 0.5, 1.0):
         p = Pool([0 if rng.random() < free_share else rng.randint(1, 3) for _ in range(blocks)], [NONE] * 3000)
-        p.fork([(0, 0, 0, 0, 1), (0, 1, 0, 0, 0), (0, 1, 0, 0, 7), (0, 100, 0, 0, 1300), (0, 2000, 0, 0, 900)])
+        p.fork([(0, 0, 0, 0, 1), (0, 1, 0, 0, 0), (0, 1, 0, 0, 7), (0, 100, 0, 0, most), (0, 2000, 0, 0, 700)])
+
+
+@gpu
+@pytest.mark.parametrize("n,entries", [(4096 // 8, 8), (1, 4096), (1, 4097), (1024, 4), (1025, 3), (1000, 1)])
+def test_records_at_the_ends_of_what_one_launch_does(n, entries):
+    rng = random.Random(n)
+    uses, table, lengths = random_pool(20000, 30, 20, rng, halves=1)
+    off = len(table)
+    records = [(rng.randrange(29) * 20, off + i * entries, c, min(entries - c, rng.randint(0, 2)), 0) for i in range(n)
+               for c in [rng.randint(0, min(entries, 20))]]
+    records = [(a, b, c, d, entries - c - d) if i % 3 else (a, b, c, d, 0) for i, (a, b, c, d, _) in enumerate(records)]
+    Pool(uses, table + [NONE] * (n * entries)).fork(records)
 
 
 @gpu
@@ -131,8 +148,28 @@ def test_sequences_go_on_from_others(n_seq, width):
         n = rng.randint(0, lengths[source])
         copied = min(n, rng.choice((0, 1, 1, 2, n)))
         records.append((source * width, (n_seq + i) * width, n - copied, copied, rng.randint(0, width - n)))
-    for fill in (0xff, 0):
-        Pool(uses, table).fork(records, work_fill=fill)
+    for fill, pad in ((0xff, 0), (0, 0), (0, min(1100, 2048 - n_seq))):
+        Pool(uses, table).fork(records, work_fill=fill, pad=pad)
+
+
+@gpu
+@both
+def test_groups_that_share_their_blocks(pad):
+    """Neighbours that name the same block at the same place, and some that do not; a source that names one block everywhere."""
+    rng = random.Random(8)
+    width = 40
+    prefix = rng.sample(range(500), 60)
+    table = [prefix[e] if e < 30 else 500 + i * width + e for i in range(20) for e in range(width)] + [NONE] * (40 * width)
+    table[7 * width:8 * width] = [3] * width
+    table[3 * width + 5], table[12 * width + 5] = NONE, 77
+    uses = [0] * 3000
+    for b in table:
+        if b != NONE:
+            uses[b] += 1
+    p = Pool(uses, table)
+    p.fork([((i if i % 5 else 7) * width, (20 + i) * width, width - 2 - i % 3, i % 3, i % 2) for i in range(20)], pad=pad)
+    p.free([(i * width, width - i % 4) for i in range(40)])
+    p.free([(i * width, width) for i in range(60)])
 
 
 @gpu
@@ -152,36 +189,38 @@ def test_pools_of_more_spans_than_one_chunk_each():
 
 
 @gpu
-def test_entries_without_a_block():
+@both
+def test_entries_without_a_block(pad):
     """None, and ids beyond the pool: shared and copied as none; what is numbered for them stays free."""
     uses = [1, 1, 0, 0, 2, 0, 0, 1]
     table = [0, NONE, 1, 8, 4, NONE, 7, 0x80000000] + [NONE] * 24
     p = Pool(uses, table)
-    assert p.fork([(0, 8, 4, 4, 2)])[1] == B.ST_BAD_BLOCK | B.ST_NO_FREE
+    assert p.fork([(0, 8, 4, 4, 2)], pad=pad)[1] == B.ST_BAD_BLOCK | B.ST_NO_FREE
     p = Pool(uses, table)
-    pairs, _ = p.fork([(0, 8, 1, 2, 0), (4, 16, 0, 2, 1)])
+    pairs, _ = p.fork([(0, 8, 1, 2, 0), (4, 16, 0, 2, 1)], pad=pad)
     assert pairs == [(NONE, NONE), (1, 3), (4, 5), (NONE, NONE)]
     p = Pool([3, 2], [0, 1, 0, NONE] + [NONE] * 8)       # nothing is free
-    assert p.fork([(0, 4, 1, 2, 1)])[0] == [(NONE, NONE)] * 2
+    assert p.fork([(0, 4, 1, 2, 1)], pad=pad)[0] == [(NONE, NONE)] * 2
 
 
 @gpu
-def test_records_that_do_not_fit():
+@both
+def test_records_that_do_not_fit(pad):
     uses, table = [1] * 10 + [0] * 50, list(range(10)) + [NONE] * 30
     for bad in [(35, 10, 4, 2, 0), (0, 36, 4, 0, 1), (0xffffffff, 10, 1, 0, 0), (0, 0xffffffff, 0, 0, 1), (0, 10, 0xffffffff, 1, 0),
                 (0, 10, 0x80000000, 0x80000000, 1), (0, 10, 0, 0, 0xffffffff), (0, 10, 3, 2, 2)]:
         p = Pool(uses, table)
-        assert p.fork([(0, 20, 2, 1, 0), bad, (4, 25, 1, 1, 3)], max_entries=6, max_pairs=9)[1] == B.ST_BAD_EXTENT, bad
+        assert p.fork([(0, 20, 2, 1, 0), bad, (4, 25, 1, 1, 3)], max_entries=6, max_pairs=9, pad=pad)[1] == B.ST_BAD_EXTENT, bad
     p = Pool(uses, table)
-    assert p.fork([(0xffffffff, 12, 0, 0, 2)])[1] == 0       # (a source that is not used)
+    assert p.fork([(0xffffffff, 12, 0, 0, 2)], pad=pad)[1] == 0       # (a source that is not used)
     for max_pairs, kept in ((0, 0), (1, 1), (2, 1), (3, 3), (4, 4)):
         p = Pool(uses, table)
-        pairs, status = p.fork([(0, 10, 2, 1, 0), (3, 15, 0, 2, 1), (5, 20, 1, 1, 0), (8, 25, 2, 0, 2)], max_pairs=max_pairs)
+        pairs, status = p.fork([(0, 10, 2, 1, 0), (3, 15, 0, 2, 1), (5, 20, 1, 1, 0), (8, 25, 2, 0, 2)], max_pairs=max_pairs, pad=pad)
         assert (len(pairs), status) == (kept, 0 if max_pairs == 4 else B.ST_BAD_EXTENT)
     p = Pool(uses, table)
-    p.fork([])
-    p.fork([(0, 10, 0, 0, 0)], max_entries=0)
-    assert p.fork([(0, 10, 1, 0, 0)], max_entries=0)[1] == B.ST_BAD_EXTENT
+    p.fork([], pad=pad)
+    p.fork([(0, 10, 0, 0, 0)], max_entries=0, pad=pad)
+    assert p.fork([(0, 10, 1, 0, 0)], max_entries=0, pad=pad)[1] == B.ST_BAD_EXTENT
 
 
 # ---------------------------------------------------------------- free
