@@ -143,11 +143,12 @@ int tutti_blocks_compact(uint32_t *d_uses, uint32_t num_blocks, uint32_t *d_bloc
   a.max_pairs = max_pairs;
   a.status = d_status;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  const auto groups = [](uint32_t things) { return std::min<uint32_t>(1024, things / 256 + (things % 256 != 0)); };
-  a.table_groups = groups(table_len);
+  // what the device holds at once: 2,048 workgroups, four things a thread
+  const auto groups = [](uint32_t things, uint32_t most) { return std::min(most, things / 256 + (things % 256 != 0)); };
+  a.table_groups = groups(table_len, 1536);
   hipLaunchKernelGGL(k_blocks_count_used, dim3(a.spans.n), dim3(256), 0, st, a);
   hipLaunchKernelGGL(k_blocks_rank, dim3(a.spans.n), dim3(256), 0, st, a);
-  hipLaunchKernelGGL(k_blocks_move, dim3(a.table_groups + groups(num_blocks)), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(k_blocks_move, dim3(a.table_groups + groups(num_blocks, 512)), dim3(256), 0, st, a);
   return launched();
 }
 

@@ -154,6 +154,12 @@ def test_values_that_are_not_finite(T, n_new, cache):
         sees = (at <= places) & ((at > places - 12) | (at < 7))
         hit = sees[:, None] & (np.arange(st.hq) // st.group == 1)
         assert np.array_equal(~np.isfinite(out[:, :, 7]), hit) and np.isfinite(np.delete(out, 7, 2)).all()
+        # keys: a NaN makes whole rows NaN, where they see it
+        st = Step([(n_new, 200 + n_new)], T=T, cache="e4m3" if cache == "e4m3" else None, d=128)
+        st.cpu.planes[0][st.table[at // T], at % T, 0, 3] = 0x7f if cache == "e4m3" else math.nan
+        out, _, _ = run_sinks(st.to_gpu(), 12, 7)
+        hit = np.broadcast_to((sees[:, None] & (np.arange(st.hq) // st.group == 0))[:, :, None], out.shape)
+        assert np.array_equal(np.isnan(out), hit), at
 
 
 @gpu
@@ -189,6 +195,28 @@ def test_records_that_cannot_be_honoured(cache):
         st.seqs = [st.seqs[0], st.seqs[2]]
         want, _, err, _, _ = sinks_reference.attend(st.cpu, st.dtype, st.seqs, st.table, st.q, st.group, 1.0 / math.sqrt(st.d), 20, 5)
         assert (np.abs(out - want) <= err).all()
+
+
+@gpu
+@pytest.mark.parametrize("cache", ["16", "e4m3"])
+@pytest.mark.parametrize("n_new", [1, 9, 70])
+@pytest.mark.parametrize("window,sinks", [(300, 70), (40, 4), (2100, 700)])
+def test_streams_of_two_thousand_million_tokens(window, sinks, n_new, cache):
+    """Close to 2^31 tokens held, all but the seen ones given back: the bits of a short sequence with the same blocks.  (Places in tiles and
+    blocks are the same, and windows say how the keys are split.)"""
+    T, far = 256, (1 << 31) - (1 << 13)
+    st = Step([(n_new, 4096 + 77)], T=T, h=2, group=2, d=64, cache="e4m3" if cache == "e4m3" else None).to_gpu()
+    near = run_sinks(st, window, sinks)
+    held = far + 77
+    table = torch.full((-(-held // T),), -1, dtype=torch.int32, device=DEV)
+    first = -(-sinks // T)
+    table[:first] = st.d_table[:first]
+    last = 4096 // T - first + 1
+    table[-last:] = st.d_table[-last:]
+    seqs = torch.tensor([[0, n_new, held, 0]], dtype=torch.int32, device=DEV)
+    st.batch = B.make_batch(seqs, 1, n_new, table, table.numel(), st.rows)
+    again = run_sinks(st, window, sinks)
+    assert same(near[0], again[0]) and same(near[1], again[1]) and near[2] == again[2] == 0 and np.isfinite(near[0]).all()
 
 
 @gpu
