@@ -33,8 +33,9 @@ struct AttendArgs {
   float *part_o;                // [part][rows][dp]: sums of weighted values
   f32x2 *part_ml;               // [part][rows]: running maximum (log2) and sum of weights
   uint32_t *status;
-  // Kernels with SINKS: the first keys, which stay visible; key tiles that a row tile sees at most; how many do not pay for a join
-  uint32_t sinks, most_tiles, whole_tiles;
+  // Kernels with SINKS: the first keys, which stay visible; key tiles that a row tile sees at most; how many do not
+  // pay for a join; what a workgroup and a join cost in tiles
+  uint32_t sinks, most_tiles, whole_tiles, unit_tiles, join_tiles;
 };
 
 // Rows of a sequence: new tokens times query heads of a KV head, in tiles of ROWS.
@@ -92,13 +93,44 @@ __device__ __forceinline__ tutti_seq record(const AttendArgs &a, const Plan &p, 
 // 164, in 256 166; of e4m3 147 in 64, 210 in 512, 357 in 2,048, whose records every workgroup reads).
 constexpr uint32_t kUnitTiles = 8;
 
+// How many tiles a part has where many sequences of few queries attend over windows (SINKS): of `rows` row tiles with `work` tiles in
+// all, the longest `most`.  Lane l weighs parts of (l + 1)/64 of the longest.  A compute unit gets through 0.61 tiles (of 8 heads) a microsecond
+// with one workgroup and 0.72 with more, so that, where row tiles are of one length, time goes by the workgroups of the fullest one of 256
+// compute units, else by all tiles and 0.6 of the last part; in tiles at 0.72, with what a workgroup and a join cost besides.  e4m3, 8 heads,
+// windows of 4,096 keys, us by this rule and by even shares or whole row tiles: 80 sequences of one length 128 and 141, 128 191 and 212, 150
+// 252 and 316; of Zipf lengths 100 125 and 134, 200 248 and 311, 300 353 and 454.  There is work memory for two rounds of slots.
+__device__ __forceinline__ uint32_t parts_of_windows(const AttendArgs &a, uint64_t work, uint64_t rows, uint32_t most) {
+  const uint32_t lane = threadIdx.x & (kLanes - 1);
+  uint32_t n = static_cast<uint32_t>((static_cast<uint64_t>(most) * (lane + 1) + kLanes - 1) / kLanes);
+  if (n < a.min_tiles) n = a.min_tiles;
+  const uint32_t parts = (most + n - 1) / n;
+  const float w = static_cast<float>(work), r = static_cast<float>(rows), t = static_cast<float>((most + parts - 1) / parts);
+  const float own = static_cast<float>(a.unit_tiles), units = static_cast<float>(a.slots / 2), limit = static_cast<float>(2 * a.slots);
+  // (as many parts as there can be, by their number and by their length; 1 in 2^20 for the roundings)
+  const bool fits = parts == 1 || r * static_cast<float>(parts) <= limit || (w / static_cast<float>(n) + r) * 1.000001f <= limit;
+  float cost;
+  if (w >= 0.9f * r * static_cast<float>(most)) {
+    cost = ceilf(r * static_cast<float>(parts) / units) * (t + own);
+    if (r * static_cast<float>(parts) <= units) cost *= 1.18f;
+  } else {
+    cost = fmaxf((w + own * (w / t + 0.5f * r)) / units + 0.6f * t, 1.18f * (t + own));
+  }
+  if (parts > 1) cost += static_cast<float>(a.join_tiles);
+  if (!fits) cost = __builtin_inff();
+  float least = cost;
+#pragma unroll
+  for (int m = 1; m < static_cast<int>(kLanes); m <<= 1) least = fminf(least, __shfl_xor(least, m, kLanes));
+  return from_lane(n, static_cast<uint32_t>(__builtin_ctzll(__ballot(cost == least))));
+}
+
 template <int ROWS, bool SINKS>
 __device__ __forceinline__ Plan make_plan(const AttendArgs &a) {
   const uint32_t lane = threadIdx.x & (kLanes - 1), head_groups = a.kv_heads / a.abreast;
   Plan p{};
   if (lane < a.batch.n_seq) p.lane_seq = load_seq(a.batch.seqs + lane);
   uint64_t work = 0;
-  uint32_t rows = 0, tiles = 0, most = 0;  // of the lane's last sequence; of all
+  uint32_t rows = 0, tiles = 0, most = 0;  // of the lane's last sequence; the largest of all
+  uint64_t rows_all = 0;
   for (uint32_t base = 0; base < a.batch.n_seq; base += kLanes) {
     if (base + lane < a.batch.n_seq) {
       const tutti_seq s = record(a, p, base, lane);
@@ -106,20 +138,28 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs &a) {
         rows = row_tiles<ROWS>(a, s) * head_groups;
         tiles = key_tiles<SINKS>(a, s);
         work += static_cast<uint64_t>(rows) * tiles;
-        if (SINKS) most = max(most, tiles);
+        if (SINKS) {
+          most = max(most, tiles);
+          rows_all += rows;
+        }
       }
     }
   }
 #pragma unroll
   for (int m = 1; m < static_cast<int>(kLanes); m <<= 1) work += __shfl_xor(work, m, kLanes);
   if constexpr (SINKS) {
-    // Row tiles stay whole where the longest one ends with the others, or little later than parts and their join would: half of the slots
-    // keep the device busy.  128 sequences of 8 heads, windows of 1,024 keys: whole 95 us, in parts 106; 40 new tokens each of 1 head:
-    // 47 and 85; but one sequence of 8 heads 68 and 24.
 #pragma unroll
-    for (int m = 1; m < static_cast<int>(kLanes); m <<= 1) most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), m, kLanes)));
-    if (most <= work / (a.slots / 2) + a.whole_tiles) {
-      p.tiles_a_part = uniform(most ? most : 1);
+    for (int m = 1; m < static_cast<int>(kLanes); m <<= 1) {
+      rows_all += __shfl_xor(rows_all, m, kLanes);
+      most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), m, kLanes)));
+    }
+    if (most == 0) most = 1;
+    // Row tiles stay whole where the longest one ends with the others, or little later than parts and their join would: half of the slots
+    // keep the device busy.  128 sequences, 40 new tokens each of 1 head, windows of 1,024 keys: whole 48 us, in parts 85; but one sequence
+    // that decodes, 8 heads, 68 and 24.
+    const bool many = ROWS < 128 && a.batch.n_seq > kLanes;
+    if (many || most <= work / (a.slots / 2) + a.whole_tiles) {
+      p.tiles_a_part = many ? parts_of_windows(a, work, rows_all, most) : uniform(most);
       return p;
     }
   }

@@ -111,10 +111,14 @@ def test_keys_in_many_parts(seqs, window, sinks, T, cache):
 
 @gpu
 @pytest.mark.parametrize("cache", ["16", "e4m3"])
-def test_more_sequences_than_lanes(cache):
-    st = Step([(1 + i % 2, 40 + 13 * i) for i in range(150)], h=2, group=2, d=64, cache="e4m3" if cache == "e4m3" else None)
-    without_hidden(st, 90, 7)
-    check_sinks(st, 90, 7)
+@pytest.mark.parametrize("n,held,window,sinks,h", [(150, lambda i: 40 + 13 * i, 90, 7, 2), (65, lambda i: 1500, 1100, 40, 1),
+                                                   (130, lambda i: 900, 700, 4, 4), (100, lambda i: 17 + 29 * i, 1300, 33, 3),
+                                                   (300, lambda i: 1 + i * i % 700, 400, 100, 4), (700, lambda i: 1 + i % 500, 300, 5, 4)])
+def test_more_sequences_than_lanes(n, held, window, sinks, h, cache):
+    """Records beyond the first 64, of one length and of many: row tiles whole and in parts, as many as there is work memory for."""
+    st = Step([(1 + i % 2 if n == 150 else 1, held(i) + 1) for i in range(n)], h=h, group=2, d=64, cache="e4m3" if cache == "e4m3" else None)
+    without_hidden(st, window, sinks)
+    check_sinks(st, window, sinks)
 
 
 @gpu
