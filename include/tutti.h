@@ -696,8 +696,9 @@ int tutti_kv_attend_sinks(const tutti_pool *pool, const tutti_scales *scales, co
 /* ---- blocks that several sequences use, and their coming and going.  A pool's blocks are counted in d_uses (device memory, 16-byte
  * aligned, num_blocks words, one array for all layers, whose tables are the same): how many table entries name a block.  A block
  * with no uses is free.  The calls below keep the counts; a table entry that names no block is TUTTI_NO_BLOCK, which they skip (the
- * calls above, where they need the block, report it as BAD_BLOCK).  They go by device memory alone, in a fixed number of launches: what a step shares, copies or gives back may
- * be decided on the GPU, and the whole step captured in a graph.  Results are the same from call to call.
+ * calls above, where they need the block, report it as BAD_BLOCK).  They go by device memory alone, in a fixed number of launches: what a
+ * step shares, copies or gives back may be decided on the GPU, and the whole step captured in a graph.  Results are the same from call
+ * to call.
  * Common to them: num_blocks below 2^31, max_entries below 2^31 and at most TUTTI_MAX_REQ records (else TUTTI_ERANGE); d_block_table of
  * table_len entries.  Calls on the same counts or tables, and the copies of blocks that they name, go in stream order. */
 #define TUTTI_NO_BLOCK 0xffffffffu /* a table entry, or a pair, that names no block */

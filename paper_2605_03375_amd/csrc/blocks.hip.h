@@ -327,7 +327,8 @@ __global__ __launch_bounds__(256) void k_blocks_fork(const ForkArgs a) {
 }
 
 // Both in one workgroup, for the few entries of a step in which sequences begin blocks or beams change places: no second launch (4 records
-// of 64 entries, a pool of 65,536 blocks: 5.8 us, the two 7.0 and a pause between them; a call 8.1 and 11.2).  Counts are read until there are enough free blocks.
+// of 64 entries, a pool of 65,536 blocks: 5.8 us, the two 7.0 and a pause between them; with the copy in front of it a call of 8.1 and 11.2).
+// Counts are read until there are enough free blocks.  Bound by its trips to memory: records and counts, tables, and what is written.
 constexpr uint32_t kSmallEntries = 4096, kSmallRecords = 1024, kSmallBlocks = 65536;
 __global__ __launch_bounds__(1024) void k_blocks_fork_small(const ForkArgs a) {
   __shared__ Fork records[kSmallRecords];
@@ -446,7 +447,7 @@ struct FreeArgs {
   uint32_t *status;
 };
 
-// An entry is taken out of the table by an exchange, so that two ranges that both have it release its block once (96 x 4 sequences, 700,000
+// An entry is taken out of the table by an exchange, so that two ranges that both have it release its block once (96 x 4 sequences, 747,000
 // entries, each block released by itself: 32.7 us, with loads and stores 31.5).  Neighbouring ranges to a workgroup: see Run.
 template <uint32_t kGroup>
 __global__ __launch_bounds__(256) void k_blocks_free(const FreeArgs a) {
@@ -625,7 +626,8 @@ struct CopyArgs {
 };
 constexpr uint32_t kPieceLoads = 4, kPiece = kPieceLoads * kLanes;
 
-// A wavefront copies a piece of 4 KiB of one plane's block; neighbours have neighbouring pieces.
+// A wavefront copies a piece of 4 KiB of one plane's block; neighbours have neighbouring pieces.  Bound by memory: 6,001 blocks of 32 KiB a
+// plane, 787 MB read and written, in 156 us, 5.0 TB/s (a contiguous copy of 1 GiB by PyTorch: 5.14).
 __global__ __launch_bounds__(256) void k_blocks_copy(const CopyArgs a) {
   const uint32_t lane = threadIdx.x & (kLanes - 1);
   const uint32_t n = a.n_pairs ? min(*constant(a.n_pairs), a.max_pairs) : a.max_pairs;

@@ -606,3 +606,23 @@ def test_the_reference_conserves_uses():
     before = sorted(u for u in uses if u)
     assert ref.compact(uses, table, 400)[1] == len(before) and sorted(uses[:len(before)]) == before
     assert ref.free(uses, table, [((10 + i) * 12, n) for i, n in enumerate(lengths)], 12) == 0 and sum(uses) == total
+
+
+def test_kernels_without_scratch():
+    from paper_2605_03375_amd import binding
+    from test_kernel_resources import BUNDLE, _code_object, _metadata, _short_names
+    with open(binding.LIB_PATH, "rb") as f:
+        blob = f.read()
+    found, at = {}, blob.find(BUNDLE)
+    while at >= 0:
+        try:
+            kernels = _metadata(_code_object(blob[at:]))["amdhsa.kernels"]
+            found.update(zip(_short_names([k[".name"] for k in kernels]), kernels))
+        except AssertionError:      # (the bundle's name is also a string of its own)
+            pass
+        at = blob.find(BUNDLE, at + 1)
+    blocks = {n: k for n, k in found.items() if n.startswith("k_blocks_")}
+    assert len(blocks) == 9
+    assert all(k[".private_segment_fixed_size"] == 0 and k[".vgpr_spill_count"] == 0 for k in blocks.values())
+    # two workgroups of 1,024 threads would have 64 registers each; the others' grids count on eight of 256
+    assert all(k[".vgpr_count"] <= 128 for k in blocks.values())

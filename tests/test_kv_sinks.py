@@ -45,12 +45,12 @@ def check_sinks(st, window, sinks, sm_scale=None, table_len=None):
     assert np.array_equal(np.isnan(out), np.broadcast_to(untouched[:, :, None], out.shape) | np.isnan(want))
     fine = np.isfinite(want)
     assert np.array_equal(out[~fine & ~np.isnan(want)], want[~fine & ~np.isnan(want)])
-    over = (np.abs(out - want) - err)[fine]
+    over = np.abs(out[fine] - want[fine]) - err[fine]
     assert over.size == 0 or over.max() <= 0, f"{over.max():.3g} beyond the bound"
     none = want_lse == -math.inf
     assert np.array_equal(lse == -math.inf, none) and np.array_equal(np.isnan(lse), untouched)
     fine = np.isfinite(want_lse)
-    assert (np.abs(lse - want_lse)[fine] <= lse_err[fine]).all()
+    assert (np.abs(lse[fine] - want_lse[fine]) <= lse_err[fine]).all()
     return out, lse
 
 
