@@ -149,12 +149,13 @@ struct AttendSizes {
   uint64_t ml_bytes, bytes;
 };
 
-int attend_sizes(const tutti_pool *pool, const tutti_batch *b, const tutti_attn *attn, AttendSizes *s) {
+// abreast: KV heads of a workgroup, 0 for as many as go with the pool
+int attend_sizes(const tutti_pool *pool, const tutti_batch *b, const tutti_attn *attn, AttendSizes *s, uint32_t abreast = 0) {
   const uint32_t group = attn->n_q_heads / pool->num_kv_heads;
   s->rows = rows_a_tile(b, group);
   s->dp = pool->head_dim <= 64 ? 64 : 128;
   if (s->rows < 128) {
-    s->abreast = heads_abreast(pool->num_kv_heads);
+    s->abreast = abreast ? abreast : heads_abreast(pool->num_kv_heads);
     s->key_waves = s->abreast == 1 ? 4 : s->abreast == 2 ? 2 : 1;
   } else {
     s->abreast = s->key_waves = 1;
@@ -182,6 +183,19 @@ uint32_t most_tiles(uint32_t rows, uint32_t group, uint32_t window, uint32_t sin
   const uint64_t places = (rows + group - 2) / group + 1, keys = window + places - 1;
   const uint64_t n = (keys + kKeyTile - 2) / kKeyTile + 1 + (static_cast<uint64_t>(sinks) + kKeyTile - 1) / kKeyTile;
   return static_cast<uint32_t>(std::min<uint64_t>(n, 0x7fffffffu));
+}
+
+// With first tokens: KV heads of a workgroup where what all windows hold is so little that the time is that of a workgroup's tiles one after the
+// other.  Then four wavefronts share a head's tiles, as long as there is a workgroup a slot at most.  One token each, four, two and one
+// heads abreast, us: e4m3, 8 heads, windows of 1,000 keys, one sequence 20.2, 14.4, 13.5, 32 sequences 30.0, 26.0, 24.2, 64 37.3, 37.5,
+// 39.0; windows of 200 keys, 32 sequences 23.0, 14.2, 11.8, 128 28.0, 20.9, 28.1 (two rounds of the slots); five heads and one, windows of
+// 4,096 keys, 32 sequences 52.4 and 42.3, 64 84.4 and 90.7.
+uint32_t heads_abreast_of_few(const tutti_pool *pool, const AttendSizes &s, uint64_t row_tiles, uint32_t tiles) {
+  const uint32_t heads = pool->num_kv_heads;
+  if (row_tiles * heads * tiles > static_cast<uint64_t>(s.slots) * (s.key_waves == 1 && s.abreast != 4 ? 48 : 24)) return s.abreast;
+  for (const uint32_t n : {1u, 2u})
+    if (n < s.abreast && heads % n == 0 && row_tiles * (heads / n) <= s.slots) return n;
+  return s.abreast == 4 || row_tiles * heads > 4 * s.slots ? s.abreast : 1;
 }
 
 int check_attn(const tutti_pool *pool, const tutti_attn *attn) {
@@ -214,6 +228,13 @@ int attend(const tutti_pool *pool, const tutti_scales *scales, const tutti_batch
   if (nothing_to_do(batch)) return TUTTI_OK;
   if (!d_work || !aligned(d_work, 16)) return TUTTI_EINVAL;
   if (work_bytes < s.bytes) return TUTTI_ERANGE;
+  const bool with_sinks = attn->window && n_sinks;  // (without a window every key stays visible)
+  const uint32_t group = attn->n_q_heads / pool->num_kv_heads;
+  const uint32_t sinks = std::min(n_sinks, 0x7fffffffu), most = with_sinks ? most_tiles(s.rows, group, attn->window, sinks) : 0;
+  if (with_sinks && s.rows < 128) {
+    const uint32_t abreast = heads_abreast_of_few(pool, s, std::min(batch->n_seq, batch->n_rows), most);  // (a row tile a sequence)
+    if (abreast != s.abreast && (rc = attend_sizes(pool, batch, attn, &s, abreast)) != TUTTI_OK) return rc;
+  }
   AttendArgs a{};
   a.pool = view(pool, scales);
   a.batch = view(batch);
@@ -221,7 +242,7 @@ int attend(const tutti_pool *pool, const tutti_scales *scales, const tutti_batch
   a.out = *out;
   a.lse = d_lse;
   a.kv_heads = pool->num_kv_heads;
-  a.group = attn->n_q_heads / pool->num_kv_heads;
+  a.group = group;
   a.d = pool->head_dim;
   a.scale_log2 = attn->sm_scale * kLog2e;
   a.causal = attn->causal;
@@ -236,9 +257,9 @@ int attend(const tutti_pool *pool, const tutti_scales *scales, const tutti_batch
   a.part_ml = reinterpret_cast<f32x2 *>(static_cast<uint8_t *>(d_work) + 16);
   a.part_o = reinterpret_cast<float *>(static_cast<uint8_t *>(d_work) + 16 + s.ml_bytes);
   a.status = d_status;
-  if (attn->window && n_sinks) {  // (without a window every key stays visible)
-    a.sinks = std::min(n_sinks, 0x7fffffffu);
-    a.most_tiles = most_tiles(s.rows, a.group, attn->window, a.sinks);
+  if (with_sinks) {
+    a.sinks = sinks;
+    a.most_tiles = most;
     a.unit_tiles = 2 * s.key_waves;
     a.join_tiles = 3 * s.key_waves;
     // So few that they are not split, by one sequence of 1 to 8 heads whole and in parts, us: one head 14 tiles 12.2 and 13.4, 27 tiles 16.3 and
