@@ -263,7 +263,7 @@ int attend(const tutti_pool *pool, const tutti_scales *scales, const tutti_batch
     a.unit_tiles = 2 * s.key_waves;
     a.join_tiles = 3 * s.key_waves;
     // So few that they are not split, by one sequence of 1 to 8 heads whole and in parts, us: one head 14 tiles 12.2 and 13.4, 27 tiles 16.3 and
-    // 13.5; two heads 10 tiles 13.7 and 13.9; eight heads 8 tiles 19.6 and 23.6, 14 tiles 32 and 24; 40 queries 8 tiles 16.6 and 16.3 to 16.8.
+    // 13.5; two heads side by side 10 tiles 13.7 and 13.9; eight, four abreast, 8 tiles 19.6 and 23.6, 14 tiles 32 and 24; 40 queries 8 tiles 16.6 and 16.3 to 16.8.
     a.whole_tiles = s.rows < 128 ? 6 + s.key_waves * 5 / 2 : 12;
     if (a.most_tiles <= a.whole_tiles) a.min_tiles = a.most_tiles;
   }

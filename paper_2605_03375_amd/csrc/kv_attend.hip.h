@@ -156,7 +156,7 @@ __device__ __forceinline__ Plan make_plan(const AttendArgs &a) {
     if (most == 0) most = 1;
     // Row tiles stay whole where the longest one ends with the others, or little later than parts and their join would: half of the slots
     // keep the device busy.  128 sequences, 40 new tokens each of 1 head, windows of 1,024 keys: whole 48 us, in parts 85; but one sequence
-    // that decodes, 8 heads, 68 and 24.
+    // that decodes, 8 heads, four abreast, 68 and 24.
     const bool many = ROWS < 128 && a.batch.n_seq > kLanes;
     if (many || most <= work / (a.slots / 2) + a.whole_tiles) {
       p.tiles_a_part = many ? parts_of_windows(a, work, rows_all, most) : uniform(most);
