@@ -222,7 +222,7 @@ __global__ __launch_bounds__(256) void k_blocks_list_free(const ForkArgs a) {
 
 // Uses that a thread adds to (takes from) a block: those of neighbouring records that name the same block at the same place, as samples of
 // one prompt do, go together.  Blocks' counts lie all over memory, and the device makes 27 such additions a nanosecond: 1,024 sequences of
-// 515,000 entries, groups of 8 that share their prompts, 24.4 us one by one, 12.5 so; 384 sequences given back, 32.7 and 11.5.
+// 515,000 entries, groups of 8 that share their prompts, 24.4 us one by one, 10.0 so; 384 sequences given back, 32.7 and 11.8.
 struct Run {
   uint32_t id, n;
 };
@@ -255,7 +255,7 @@ __device__ __forceinline__ uint32_t put_entry(const ForkArgs &a, const Fork &f, 
 
 // The second: the same chunk of entries of kGroup neighbouring records to a workgroup.  New block number k lies in the span whose free
 // blocks are numbered around it: a search in LDS over the sums of the spans' counts.
-constexpr uint32_t kGroup = 8;
+constexpr uint32_t kGroup = 4;   // (the 1,024 sequences: 4 together 10.0 us, 8 11.5, 16 18.8)
 __global__ __launch_bounds__(256) void k_blocks_fork(const ForkArgs a) {
   __shared__ __attribute__((aligned(16))) uint32_t before[kMostSpans];
   __shared__ uint32_t sums[4];
