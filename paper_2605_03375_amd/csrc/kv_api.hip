@@ -233,7 +233,8 @@ int attend(const tutti_pool *pool, const tutti_scales *scales, const tutti_batch
   const uint32_t sinks = std::min(n_sinks, 0x7fffffffu), most = with_sinks ? most_tiles(s.rows, group, attn->window, sinks) : 0;
   if (with_sinks && s.rows < 128) {
     const uint32_t abreast = heads_abreast_of_few(pool, s, std::min(batch->n_seq, batch->n_rows), most);  // (a row tile a sequence)
-    if (abreast != s.abreast && (rc = attend_sizes(pool, batch, attn, &s, abreast)) != TUTTI_OK) return rc;
+    AttendSizes few;  // (more workgroups: rows that no sequence has may make them too many for a launch)
+    if (abreast != s.abreast && attend_sizes(pool, batch, attn, &few, abreast) == TUTTI_OK) s = few;
   }
   AttendArgs a{};
   a.pool = view(pool, scales);

@@ -224,6 +224,24 @@ def test_streams_of_two_thousand_million_tokens(window, sinks, n_new, cache):
 
 
 @gpu
+def test_rows_that_no_sequence_has():
+    """So many that workgroups of one head would be too many for a launch, and those of four are not: the same results."""
+    st = Step([(1, 700), (1, 90)], h=8, group=1, d=64).to_gpu()
+    want = run_sinks(st, 100, 5)
+    n = 1 << 26
+    attn = B.make_attn(st.hq, B.BF16, 1.0 / math.sqrt(st.d), window=100)
+    batch = B.make_batch(st.d_seqs, 2, 1, st.d_table, st.d_table.numel(), n)
+    out, lse = torch.empty((st.rows, st.hq, st.d), dtype=torch.bfloat16, device=DEV), torch.empty((st.rows, st.hq), device=DEV)
+    work = torch.empty(B.tutti_kv_attend_work_bytes(st.pool, batch, attn), dtype=torch.uint8, device=DEV)
+    B.tutti_kv_attend_sinks(st.pool, None, batch, attn, 5, B.make_rows(st.d_q), B.make_rows(out), lse, work, work.numel(), st.status)
+    torch.cuda.synchronize()
+    ref_out, ref_lse, err, lse_err, _ = sinks_reference.attend(st.cpu, st.dtype, st.seqs, st.table, st.q, 1, 1.0 / math.sqrt(st.d), 100, 5)
+    for got_out, got_lse in ((out.float().cpu().numpy(), lse.cpu().numpy()), want[:2]):
+        assert (np.abs(got_out - ref_out) <= err).all() and (np.abs(got_lse - ref_lse) <= lse_err).all()
+    assert int(st.status.item()) == 0
+
+
+@gpu
 def test_twice_the_same_on_another_stream_and_in_a_graph():
     st = Step([(1, 3000), (1, 500), (2, 400)], h=8, d=128, cache="e4m3").to_gpu()
     want = run_sinks(st, 1500, 100)
