@@ -703,7 +703,8 @@ int tutti_kv_attend_sinks(const tutti_pool *pool, const tutti_scales *scales, co
  * table_len entries.  Calls on the same counts or tables, and the copies of blocks that they name, go in stream order. */
 #define TUTTI_NO_BLOCK 0xffffffffu /* a table entry, or a pair, that names no block */
 #define TUTTI_ST_NO_FREE 64u   /* tutti_blocks_fork: fewer free blocks than asked for: the entry is TUTTI_NO_BLOCK */
-#define TUTTI_ST_BAD_USES 128u /* tutti_blocks_free: a block that has no uses was to be given back: its count stays 0 */
+#define TUTTI_ST_BAD_USES 128u /* a table entry names a block that has no uses.  tutti_blocks_free: its count stays 0.
+                                * tutti_blocks_fork: nobody goes on from it */
 
 /* Where a sequence goes on from another's blocks, or grows: table entries [dst_off, dst_off + n_shared + n_copied + n_new) <-
  * n_shared blocks that it shares (entries from src_off on; a use more for each), n_copied blocks of its own into which those named by
@@ -727,7 +728,7 @@ typedef struct tutti_block_range {
 
 /* Fork.  The copied and new blocks of all records, in order, are numbered; number k gets the free block with the k-th lowest id (free
  * when the call begins), one use.  Entries of the source that name no block are shared or copied as TUTTI_NO_BLOCK (those >=
- * num_blocks too, BAD_BLOCK), and their number's block stays free.  d_pairs[p] <- (source's block, its copy) for the p-th copied
+ * num_blocks too, BAD_BLOCK, and those that name a free block, BAD_USES), and their number's block stays free.  d_pairs[p] <- (source's block, its copy) for the p-th copied
  * entry of all records, (TUTTI_NO_BLOCK, TUTTI_NO_BLOCK) where there is no copy to make; *d_n_pairs (may be NULL) <- how many.  The caller
  * has them copied in every layer (tutti_blocks_copy) before the sequences go on.
  * Skipped with BAD_EXTENT, nothing of theirs written or numbered: records with more than max_entries entries, and those whose

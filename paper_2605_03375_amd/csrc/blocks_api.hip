@@ -40,6 +40,7 @@ int check_table(const uint32_t *uses, uint32_t num_blocks, const uint32_t *table
 }
 
 uint64_t list_bytes(uint32_t num_blocks) { return (static_cast<uint64_t>(num_blocks) * 4 + 15) / 16 * 16; }
+uint64_t bits_bytes(uint32_t num_blocks) { return (static_cast<uint64_t>(num_blocks) + 127) / 128 * 16; }
 
 }  // namespace
 
@@ -47,7 +48,7 @@ extern "C" {
 
 uint64_t tutti_blocks_fork_work_bytes(uint32_t num_blocks, uint32_t n_forks) {
   if (num_blocks == 0 || num_blocks >= kMostThings || n_forks > TUTTI_MAX_REQ) return 0;
-  return kMostSpans * 4 + static_cast<uint64_t>(n_forks) * sizeof(u32x2) + 16 + list_bytes(num_blocks);
+  return kMostSpans * 4 + static_cast<uint64_t>(n_forks) * sizeof(u32x2) + 16 + list_bytes(num_blocks) + bits_bytes(num_blocks);
 }
 
 int tutti_blocks_fork(uint32_t *d_uses, uint32_t num_blocks, uint32_t *d_block_table, uint32_t table_len, const tutti_fork *d_forks,
@@ -68,6 +69,7 @@ int tutti_blocks_fork(uint32_t *d_uses, uint32_t num_blocks, uint32_t *d_block_t
   a.spans = spans_of(d_uses, num_blocks, reinterpret_cast<uint32_t *>(work));
   a.first = reinterpret_cast<u32x2 *>(work + kMostSpans * 4);
   a.list = reinterpret_cast<uint32_t *>(work + kMostSpans * 4 + (static_cast<uint64_t>(n_forks) * sizeof(u32x2) + 15) / 16 * 16);
+  a.free = a.list + list_bytes(num_blocks) / 4;
   a.uses = d_uses;
   a.table = d_block_table;
   a.table_len = table_len;

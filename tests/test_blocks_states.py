@@ -1,0 +1,92 @@
+"""Tables, counts and pools that tutti_blocks_* can meet beside those of test_blocks: entries that name free blocks, and sizes at which every
+loop of a kernel goes round again.  On the GPU, against the definitions, to the last bit."""
+import random
+
+import numpy as np
+import pytest
+import torch
+
+import blocks_reference as ref
+from paper_2605_03375_amd import binding as B
+from test_blocks import DEV, NONE, Pool, back, both, gpu, random_pool, words
+
+
+# ---------------------------------------------------------------- entries that name free blocks
+
+def fork_from_used(uses, table, records, max_entries, max_pairs):
+    """ref.fork, where sources' entries that name a block without uses are taken as entries that name none."""
+    stale = [b < len(uses) and uses[b] == 0 for b in table]
+    named = [NONE if s else b for s, b in zip(stale, table)]
+    mine, hit = list(named), False
+    pairs, status = ref.fork(uses, mine, records, max_entries, max_pairs)
+    written = set()
+    for src, dst, shared, copied, new in records:
+        hit |= any(stale[src:src + shared + copied])
+        written.update(range(dst, dst + shared + copied + new))
+    for e in range(len(table)):
+        if e in written:
+            table[e] = mine[e]
+    return pairs, status | (B.ST_BAD_USES if hit else 0)
+
+
+def check_fork(uses, table, records, pad=0):
+    """The call against fork_from_used; returns the pairs."""
+    records = records + [(0, 0, 0, 0, 0)] * pad
+    p = Pool(uses, table)
+    max_pairs, most = sum(r[3] for r in records), max([sum(r[2:]) for r in records] + [1])
+    rec = np.zeros(len(records), B.FORK_DTYPE)
+    for i, r in enumerate(records):
+        rec[i] = (*r, (9, 9, 9))
+    pairs, n_pairs = words([3] * (2 * max_pairs + 2)), words([3])
+    need = B.tutti_blocks_fork_work_bytes(len(uses), len(records))
+    work = torch.full((need + 16,), 0xff, dtype=torch.uint8, device=DEV)
+    B.tutti_blocks_fork(p.d_uses, len(uses), p.d_table, len(table), words(rec.view(np.uint32)), len(records), most, pairs, n_pairs, max_pairs,
+                        work, need, p.d_status)
+    want, status = fork_from_used(p.uses, p.table, records, most, max_pairs)
+    p.check(status)
+    assert back(n_pairs) == [len(want)] and back(pairs) == [x for q in want for x in q] + [3, 3]
+    assert bool((work[need:] == 0xff).all())
+    return want, status
+
+
+def test_the_reference_leaves_free_blocks_alone():
+    """What goes wrong without: the free block that an entry names is handed out in the same call, and has two owners."""
+    uses, table = [1, 0, 0, 1], [0, 1, 3] + [NONE] * 6
+    a, b = list(uses), list(table)
+    ref.fork(a, b, [(0, 3, 3, 0, 0), (0, 6, 0, 0, 2)], 3, 0)
+    assert b[4] == b[6] == 1 and a[1] == 2
+    a, b = list(uses), list(table)
+    assert fork_from_used(a, b, [(0, 3, 3, 0, 0), (0, 6, 0, 0, 2)], 3, 0) == ([], B.ST_BAD_USES)
+    assert b[:8] == [0, 1, 3, 0, NONE, 3, 1, 2] and a == [2, 1, 1, 2]
+
+
+@gpu
+@both
+def test_fork_from_free_blocks(pad):
+    uses, table = [1, 0, 0, 1, 0, 0], [0, 1, 3] + [NONE] * 20
+    check_fork(uses, table, [(0, 3, 3, 0, 0), (0, 6, 0, 0, 2)], pad)                 # shared; handed out by the second record
+    pairs, status = check_fork(uses, table, [(0, 3, 1, 2, 0), (0, 8, 0, 3, 1)], pad)   # copied: no pair has it as its source
+    assert pairs == [(NONE, NONE), (3, 2), (0, 4), (NONE, NONE)] + [(NONE, NONE)] and status == B.ST_BAD_USES | B.ST_NO_FREE
+    check_fork([0] * 6, [0, 1, 2, 3, 4, 5] + [NONE] * 20, [(0, 6, 3, 3, 0), (0, 12, 0, 6, 2)], pad)
+    check_fork([2], [0, 0, 0] + [NONE] * 6, [(0, 3, 2, 1, 0)], pad)
+
+
+@gpu
+@pytest.mark.parametrize("blocks", [3, 64, 65, 1000, 65536, 65537, 70001, (1 << 20) + 1500])
+@pytest.mark.parametrize("n_seq,width,pad", [(4, 64, 0), (4, 64, 1100), (70, 90, 0), (3, 1500, 0)])
+def test_some_of_the_entries_name_free_blocks(blocks, n_seq, width, pad):
+    """Both kernels; the pool's last blocks; neighbours that share; every word of the bits."""
+    rng = np.random.default_rng(blocks)
+    uses = (rng.random(blocks) < 0.8).astype(int) * rng.integers(1, 3, blocks)
+    uses[-3:] = [0, 1, 0]
+    table = rng.integers(0, blocks, n_seq * width)
+    table[rng.random(table.size) < 0.1] = NONE
+    table[::7] = blocks - 1 - np.arange(table[::7].size) % 3
+    for i in range(1, n_seq, 3):
+        table[i * width:i * width + width // 2] = table[(i - 1) * width:(i - 1) * width + width // 2]
+    records = []
+    for i in range(n_seq):
+        n = int(rng.integers(0, width + 1))
+        copied = int(min(n, rng.integers(0, 5)))
+        records.append((i * width, (n_seq + i) * width, n - copied, copied, int(min(width - n, rng.integers(0, 3)))))
+    check_fork(uses.tolist(), table.tolist() + [NONE] * (n_seq * width), records, pad)
