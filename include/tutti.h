@@ -704,7 +704,7 @@ int tutti_kv_attend_sinks(const tutti_pool *pool, const tutti_scales *scales, co
 #define TUTTI_NO_BLOCK 0xffffffffu /* a table entry, or a pair, that names no block */
 #define TUTTI_ST_NO_FREE 64u   /* tutti_blocks_fork: fewer free blocks than asked for: the entry is TUTTI_NO_BLOCK */
 #define TUTTI_ST_BAD_USES 128u /* a table entry names a block that has no uses.  tutti_blocks_free: its count stays 0.
-                                * tutti_blocks_fork: nobody goes on from it */
+                                * tutti_blocks_fork: nobody goes on from it.  tutti_blocks_compact: the entry is TUTTI_NO_BLOCK */
 
 /* Where a sequence goes on from another's blocks, or grows: table entries [dst_off, dst_off + n_shared + n_copied + n_new) <-
  * n_shared blocks that it shares (entries from src_off on; a use more for each), n_copied blocks of its own into which those named by
@@ -753,7 +753,9 @@ int tutti_blocks_free(uint32_t *d_uses, uint32_t num_blocks, uint32_t *d_block_t
  * lies at n or behind it: the used ones are then the first n.  d_pairs[k] <- (from, to), and their counts move; every table entry
  * that names one follows, whoever it belongs to.  d_totals[0] <- moves, d_totals[1] <- n.  At most max_pairs moves are made (there
  * are never more than num_blocks / 2).  The caller has the blocks copied in every layer (tutti_blocks_copy: no block is both a
- * source and a destination) before anything uses the table.  Entries >= num_blocks stay (BAD_BLOCK, but for TUTTI_NO_BLOCK).
+ * source and a destination) before anything uses the table.  Entries >= num_blocks stay (BAD_BLOCK, but for TUTTI_NO_BLOCK), and so
+ * do those that name a free block at n or behind it; those that name a free block below n become TUTTI_NO_BLOCK (BAD_USES): what moves
+ * there is not theirs.
  * d_work as for tutti_blocks_fork. */
 uint64_t tutti_blocks_compact_work_bytes(uint32_t num_blocks);
 int tutti_blocks_compact(uint32_t *d_uses, uint32_t num_blocks, uint32_t *d_block_table, uint32_t table_len,

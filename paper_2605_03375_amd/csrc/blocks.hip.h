@@ -529,6 +529,8 @@ struct CompactArgs {
   uint32_t max_pairs;
   uint32_t *holes;   // free blocks in front of the end, in order
   uint32_t *rank;    // of a used block behind the end: how many used ones are behind it; kNoBlock for free ones
+  uint32_t *used;    // a bit for each block; behind `rank`, `used_at` words from there
+  uint32_t used_at;
   uint32_t *found;   // holes, used blocks
   uint32_t table_groups;
   uint32_t *status;
@@ -566,6 +568,7 @@ __global__ __launch_bounds__(256) void k_blocks_rank(const CompactArgs a) {
   for (uint32_t in = 0; in < s.size && in < s.num_blocks - begin; in += kChunk) {
     if (in) u = chunk_uses(s, begin + in);
     const Marked m = mark(s, begin + in, u, true, stretches);
+    keep_bits(s, begin + in, m, a.used);
 #pragma unroll
     for (uint32_t i = 0; i < 4; ++i) {
       const uint32_t b = begin + in + i * 256 + threadIdx.x;
@@ -592,7 +595,7 @@ __global__ __launch_bounds__(256) void k_blocks_move(const CompactArgs a) {
   // Four things a thread at a time, apart by the grid's width: what an entry names, where that is listed and where it goes are trips to
   // memory one after the other.
   if (blockIdx.x < a.table_groups) {
-    bool bad = false;
+    uint32_t bad = 0;
     const uint64_t step = static_cast<uint64_t>(a.table_groups) * 256;
     for (uint64_t from = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; from < a.table_len; from += 4 * step) {
       uint32_t b[4], r[4];
@@ -600,14 +603,24 @@ __global__ __launch_bounds__(256) void k_blocks_move(const CompactArgs a) {
       for (uint32_t i = 0; i < 4; ++i) b[i] = from + i * step < a.table_len ? a.table[from + i * step] : kNoBlock;
 #pragma unroll
       for (uint32_t i = 0; i < 4; ++i) {
-        bad |= b[i] >= a.spans.num_blocks && b[i] != kNoBlock;
-        r[i] = b[i] >= end && b[i] < a.spans.num_blocks ? a.rank[b[i]] : kNoBlock;
+        if (b[i] >= a.spans.num_blocks && b[i] != kNoBlock) bad |= TUTTI_ST_BAD_BLOCK;
+        // (a block's rank or its word of bits: one load)
+        r[i] = b[i] < a.spans.num_blocks ? a.rank[b[i] >= end ? b[i] : a.used_at + b[i] / 32] : kNoBlock;
       }
 #pragma unroll
-      for (uint32_t i = 0; i < 4; ++i)
-        if (r[i] < moves) a.table[from + i * step] = a.holes[r[i]];
+      for (uint32_t i = 0; i < 4; ++i) {
+        if (b[i] < end) {
+          // an entry that names a hole must not name what moves there
+          if (!(r[i] >> (b[i] % 32) & 1u)) {
+            a.table[from + i * step] = kNoBlock;
+            bad |= TUTTI_ST_BAD_USES;
+          }
+        } else if (r[i] < moves) {
+          a.table[from + i * step] = a.holes[r[i]];
+        }
+      }
     }
-    if (bad) report(a.status, TUTTI_ST_BAD_BLOCK);
+    if (bad) report(a.status, bad);
     return;
   }
   // used blocks behind the end

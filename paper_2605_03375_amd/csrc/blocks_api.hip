@@ -121,7 +121,7 @@ int tutti_blocks_free(uint32_t *d_uses, uint32_t num_blocks, uint32_t *d_block_t
 
 uint64_t tutti_blocks_compact_work_bytes(uint32_t num_blocks) {
   if (num_blocks == 0 || num_blocks >= kMostThings) return 0;
-  return kMostSpans * 4 + 16 + 2 * list_bytes(num_blocks);
+  return kMostSpans * 4 + 16 + 2 * list_bytes(num_blocks) + bits_bytes(num_blocks);
 }
 
 int tutti_blocks_compact(uint32_t *d_uses, uint32_t num_blocks, uint32_t *d_block_table, uint32_t table_len,
@@ -137,6 +137,8 @@ int tutti_blocks_compact(uint32_t *d_uses, uint32_t num_blocks, uint32_t *d_bloc
   a.found = reinterpret_cast<uint32_t *>(work + kMostSpans * 4);
   a.holes = reinterpret_cast<uint32_t *>(work + kMostSpans * 4 + 16);
   a.rank = reinterpret_cast<uint32_t *>(work + kMostSpans * 4 + 16 + list_bytes(num_blocks));
+  a.used_at = static_cast<uint32_t>(list_bytes(num_blocks) / 4);
+  a.used = a.rank + a.used_at;
   a.uses = d_uses;
   a.table = d_block_table;
   a.table_len = table_len;

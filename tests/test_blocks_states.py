@@ -90,3 +90,49 @@ def test_some_of_the_entries_name_free_blocks(blocks, n_seq, width, pad):
         copied = int(min(n, rng.integers(0, 5)))
         records.append((i * width, (n_seq + i) * width, n - copied, copied, int(min(width - n, rng.integers(0, 3)))))
     check_fork(uses.tolist(), table.tolist() + [NONE] * (n_seq * width), records, pad)
+
+
+def compact_used(uses, table, max_pairs):
+    """ref.compact, after which entries that named a hole name no block."""
+    n = sum(u != 0 for u in uses)
+    holes = [e for e, b in enumerate(table) if b < n and uses[b] == 0]
+    pairs, n, status = ref.compact(uses, table, max_pairs)
+    for e in holes:
+        table[e] = NONE
+    return pairs, n, status | (B.ST_BAD_USES if holes else 0)
+
+
+def check_compact(uses, table, max_pairs):
+    p = Pool(uses, table)
+    pairs, totals = words([3] * (2 * max_pairs + 2)), words([3, 3, 3])
+    need = B.tutti_blocks_compact_work_bytes(len(uses))
+    work = torch.full((need + 16,), 0xff, dtype=torch.uint8, device=DEV)
+    B.tutti_blocks_compact(p.d_uses, len(uses), p.d_table, len(table), pairs, totals, max_pairs, work, need, p.d_status)
+    want, n, status = compact_used(p.uses, p.table, max_pairs)
+    p.check(status)
+    assert back(totals) == [len(want), n, 3] and bool((work[need:] == 0xff).all())
+    assert back(pairs) == [x for q in want for x in q] + [3] * (2 * (max_pairs - len(want)) + 2)
+    return want, status
+
+
+def test_the_reference_does_not_give_a_hole_s_entry_what_moves_there():
+    uses, table = [1, 0, 0, 1], [0, 1, 2, 3]
+    a, b = list(uses), list(table)
+    ref.compact(a, b, 2)
+    assert b[1] == b[3] == 1 and a[1] == 1                 # two entries, one use
+    a, b = list(uses), list(table)
+    assert compact_used(a, b, 2) == ([(3, 1)], 2, B.ST_BAD_USES) and b == [0, NONE, 2, 1]
+
+
+@gpu
+@pytest.mark.parametrize("blocks", [1, 2, 5, 64, 65, 1000, 1025, 40003, (1 << 20) + 1500])
+def test_compact_with_entries_that_name_free_blocks(blocks):
+    """Holes, whether something moves into them or not; free blocks behind the used ones; the pool's last blocks."""
+    rng = np.random.default_rng(blocks)
+    for share in (0.0, 0.03, 0.5, 0.97, 1.0):
+        uses = ((rng.random(blocks) < share) * rng.integers(1, 4, blocks)).tolist()
+        table = rng.integers(0, blocks, 3000)
+        table[::9] = blocks - 1 - np.arange(table[::9].size) % min(blocks, 70)
+        table[rng.random(table.size) < 0.1] = NONE
+        for most in {0, 1, blocks // 5, blocks // 2}:
+            check_compact(uses, table.tolist(), most)
