@@ -25,7 +25,7 @@ SOURCES += [os.path.join(CSRC, f"kv_attend_{q}{pool}{kind}.hip")
             for q in ("bf16", "fp16") for pool in ("", "_e4m3") for kind in ("", "_sinks")]
 DEPS = SOURCES + [os.path.join(CSRC, "tutti_kernels.hip.h"), os.path.join(CSRC, "launch_rules.h"),
                   os.path.join(CSRC, "layer_call.h"), os.path.join(CSRC, "library_state.h"),
-                  os.path.join(CSRC, "kv_common.hip.h"), os.path.join(CSRC, "kv_append.hip.h"),
+                  os.path.join(CSRC, "kv_common.hip.h"), os.path.join(CSRC, "kv_append.hip.h"), os.path.join(CSRC, "attend_rules.h"),
                   os.path.join(CSRC, "blocks.hip.h"), os.path.join(CSRC, "kv_attend.hip.h"), os.path.join(CSRC, "kv_attend_launch.h"),
                   os.path.join(CSRC, "kv_attend_launch.hip.h"),
                   os.path.join(ROOT, "include", "tutti.h"),

@@ -2,11 +2,11 @@
 #pragma once
 #include <type_traits>
 
+#include "attend_rules.h"
 #include "kv_common.hip.h"
 
 namespace tutti {
 
-constexpr uint32_t kKeyTile = 32;    // keys that a wavefront takes at a time: two halves of 16
 constexpr uint32_t kMostWaves = 5;   // wavefronts of a workgroup at most
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 // A row's running maximum is raised only by steps of more than this (log2): until then nothing that has been summed has to be rescaled.
