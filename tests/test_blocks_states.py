@@ -136,3 +136,88 @@ def test_compact_with_entries_that_name_free_blocks(blocks):
         table[rng.random(table.size) < 0.1] = NONE
         for most in {0, 1, blocks // 5, blocks // 2}:
             check_compact(uses, table.tolist(), most)
+
+
+# ---------------------------------------------------------------- sizes at which loops go round again
+
+def follow(uses, table, max_pairs):
+    """ref.compact for large pools: pairs, and uses and table as they are afterwards."""
+    blocks = uses.size
+    n = int((uses != 0).sum())
+    holes, movers = np.flatnonzero(uses[:n] == 0), n + np.flatnonzero(uses[n:])[::-1]
+    k = min(max_pairs, holes.size)
+    holes, movers = holes[:k], movers[:k]
+    to = np.arange(blocks)
+    to[movers] = holes
+    uses = uses.copy()
+    uses[holes] = uses[movers]
+    uses[movers] = 0
+    named = table != NONE
+    return np.stack([movers, holes], 1), n, uses, np.where(named, to[np.where(named, table, 0)], NONE)
+
+
+def test_large_pools_follow_the_reference():
+    rng = random.Random(3)
+    uses, table, _ = random_pool(500, 12, 20, rng)
+    for most in (0, 3, 250):
+        pairs, n, u, t = follow(np.array(uses), np.array(table), most)
+        a, b = list(uses), list(table)
+        want, m, status = ref.compact(a, b, most)
+        assert (pairs.tolist(), n, u.tolist(), t.tolist(), status) == ([list(p) for p in want], m, a, b, 0)
+
+
+@gpu
+@pytest.mark.parametrize("blocks,share,entries", [(2_000_003, 0.3, 5_000_001), (1_300_000, 0.55, 1_572_865), (600_001, 0.01, 3_200_000)])
+def test_compaction_of_more_than_a_grid_takes_at_once(blocks, share, entries):
+    """Tables of more than 1,572,864 entries, more than 524,288 blocks behind the used ones' end; thousands of chunks."""
+    rng = np.random.default_rng(blocks)
+    uses = (rng.random(blocks) < share) * rng.integers(1, 5, blocks)
+    uses[-1] = 1
+    used = np.flatnonzero(uses)
+    table = used[rng.integers(0, used.size, entries)]
+    table[rng.random(entries) < 0.05] = NONE
+    table[-1] = table[0] = blocks - 1
+    for most in (blocks // 2, 1000):
+        d_uses, d_table, status = words(uses), words(table), torch.zeros(1, dtype=torch.int32, device=DEV)
+        pairs, totals = words([3] * (2 * most)), words([3, 3])
+        work = torch.full((B.tutti_blocks_compact_work_bytes(blocks),), 0xff, dtype=torch.uint8, device=DEV)
+        B.tutti_blocks_compact(d_uses, blocks, d_table, entries, pairs, totals, most, work, work.numel(), status)
+        torch.cuda.synchronize()
+        want, n, u, t = follow(uses, table, most)
+        assert totals.tolist() == [len(want), n] and int(status.item()) == 0
+        assert torch.equal(pairs[:want.size].cpu(), words(want.ravel()).cpu()) and bool((pairs[want.size:] == 3).all())
+        assert torch.equal(d_uses, words(u)) and torch.equal(d_table, words(t))
+
+
+@gpu
+@pytest.mark.parametrize("T,h,d,gap,blocks,n", [(16, 2, 64, 0, 12000, 5000),      # one piece of 4 KiB a block
+                                                (10, 4, 128, 48, 8000, 3001),     # three pieces, the last one half
+                                                (4096, 40, 128, 16, 5, 2),        # 10,240 pieces
+                                                (1, 1, 16, 0, 30000, 14999)])     # two lanes' loads
+def test_copies_of_more_than_a_grid_takes_at_once(T, h, d, gap, blocks, n):
+    """Where the number of pairs lies on the device 8,192 pieces are copied at a time: each once, with its scales, and nothing else."""
+    stride = T * h * d * 2 + gap
+    assert 2 * n * -(-T * h * d * 2 // 4096) > 8192
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(n)
+    planes = [torch.randint(-2 ** 62, 2 ** 62, (blocks * stride // 8,), generator=gen, device=DEV) for _ in range(2)]
+    scales = [torch.randn(blocks, h + 2, device=DEV) for _ in range(2)]
+    pool = B.make_pool(*planes, num_blocks=blocks, block_tokens=T, num_kv_heads=h, head_dim=d, elt_bytes=2, block_stride=stride)
+    order = np.random.default_rng(n).permutation(blocks)
+    pairs = np.stack([order[:n], order[n:2 * n]], 1)
+    pairs[n // 2] = NONE
+    real = np.delete(pairs, n // 2, 0)
+    src, dst = (torch.from_numpy(real[:, i].astype(np.int64)).to(DEV) for i in range(2))
+    size = (stride - gap) // 8
+    want = [p.clone() for p in planes]
+    for x in want:
+        x = x.view(blocks, stride // 8)
+        x[dst, :size] = x[src, :size]
+    want_s = [s.clone() for s in scales]
+    for x in want_s:
+        x[dst, :h] = x[src, :h]
+    spare = np.stack([order[2 * n:2 * n + 1], order[2 * n:2 * n + 1]], 1)      # behind what the device says there is
+    d_pairs, status = words(np.concatenate([pairs, spare])), torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.tutti_blocks_copy(pool, B.make_scales(*scales), d_pairs, words([n]), len(pairs) + len(spare), status)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(planes + scales, want + want_s)) and int(status.item()) == 0

@@ -1,13 +1,16 @@
 """Attention over a window and first tokens with several KV heads side by side in a workgroup: that the rule takes each of its choices in
 these cases (CPU), and each choice against 64-bit definitions (GPU)."""
 import ctypes
+import math
 import os
 import subprocess
 
 import pytest
+import torch
 
-from test_kv_ops import Step
-from test_kv_sinks import check_sinks, gpu, without_hidden
+from paper_2605_03375_amd import binding as B
+from test_kv_ops import DEV, Step
+from test_kv_sinks import DTYPE, check_sinks, gpu, without_hidden
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 SOURCE = """
@@ -113,3 +116,27 @@ def test_heads_side_by_side(name, cache):
     st = Step(seqs, cache="e4m3" if cache == "e4m3" else None, seed=len(seqs) + window, **shape)
     without_hidden(st, window, sinks)
     check_sinks(st, window, sinks)
+
+
+def tiles_a_part(st, window, sinks):
+    """What the kernel put in front of its work memory: key tiles of 32 that a part has."""
+    out = torch.empty(st.rows, st.hq, st.d, dtype=st.d_q.dtype, device=DEV)
+    attn = B.make_attn(st.hq, DTYPE[st.dtype], 1.0 / math.sqrt(st.d), window=window)
+    work = torch.empty(B.tutti_kv_attend_work_bytes(st.pool, st.batch, attn) // 4, dtype=torch.int32, device=DEV)
+    B.tutti_kv_attend_sinks(st.pool, st.scales, st.batch, attn, sinks, B.make_rows(st.d_q), B.make_rows(out), None, work, work.numel() * 4)
+    return int(work[0].item())
+
+
+@gpu
+@pytest.mark.parametrize("cache", ["16", "e4m3"])
+@pytest.mark.parametrize("seqs,shape,window", [
+    ([(700, 2600)], dict(h=4, group=4, d=64), 1500),                                     # tiles of 128 rows
+    (uneven(40, 3000, 1) + even(36, 2900, 8), dict(h=8, group=4, d=64), 2600)])          # of 32, more than 64 sequences
+def test_more_joined_rows_than_a_grid_takes_at_once(seqs, shape, window, cache):
+    """More than 8,192 rows of sequences that are split: the join goes round again."""
+    st = Step(seqs, cache="e4m3" if cache == "e4m3" else None, seed=9, **shape)
+    without_hidden(st, window, 10)
+    check_sinks(st, window, 10)
+    a_part = tiles_a_part(st, window, 10)
+    seen = [min(held, window + 7) // 32 for _, held in seqs]
+    assert sum(new * st.hq for (new, _), n in zip(seqs, seen) if n > a_part) > 8192, a_part
