@@ -688,7 +688,11 @@ int tutti_kv_attend(const tutti_pool *pool, const tutti_scales *scales, const tu
  * sequence.  Query i, at place p, sees key j if j < n_held and j <= p and (j > p - window or j < n_sinks).  Blocks in which no query
  * of the step sees a key are not looked up: their table entries may name anything (TUTTI_NO_BLOCK once tutti_blocks_free has given
  * them back), and nothing is reported for them.  n_sinks = 0, or attn->window = 0 (all keys are seen): as tutti_kv_attend.
- * Everything else, the size of the work memory included, is as there. */
+ * Everything else, the size of the work memory included, is as there.
+ * Keys are taken as they lie in the cache: tutti_kv_append has rotated them by their tokens' places in the whole sequence (or by the
+ * positions given with them), and nothing rotates them again.  So the distance between a query and the first tokens grows with the
+ * sequence, whose positions have to stay below n_pos; what counts places inside the cache, with the window's tokens right behind the first
+ * ones, is another operator. */
 int tutti_kv_attend_sinks(const tutti_pool *pool, const tutti_scales *scales, const tutti_batch *batch, const tutti_attn *attn,
                           uint32_t n_sinks, const tutti_rows *q, const tutti_rows *out, float *d_lse, void *d_work,
                           uint64_t work_bytes, uint32_t *d_status, void *stream);

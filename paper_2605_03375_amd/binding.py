@@ -837,7 +837,8 @@ def tutti_kv_attend(pool, scales, batch, attn, q, out, d_lse, d_work, work_bytes
 
 
 def tutti_kv_attend_sinks(pool, scales, batch, attn, n_sinks, q, out, d_lse, d_work, work_bytes, d_status=None, stream=None):
-    """tutti_kv_attend whose queries see the first n_sinks tokens of their sequences beside attn's window."""
+    """tutti_kv_attend whose queries see the first n_sinks tokens of their sequences beside attn's window (keys as they were appended,
+    rotated by their places in the whole sequence)."""
     return _check("tutti_kv_attend_sinks", lib().tutti_kv_attend_sinks(_ref(pool), _ref(scales), _ref(batch), _ref(attn), n_sinks,
                                                                        _ref(q), _ref(out), _p(d_lse), _p(d_work), work_bytes,
                                                                        _p(d_status), _stream(stream)))

@@ -1,5 +1,6 @@
 """Tables, counts and pools that tutti_blocks_* can meet beside those of test_blocks: entries that name free blocks, and sizes at which every
 loop of a kernel goes round again.  On the GPU, against the definitions, to the last bit."""
+import math
 import random
 
 import numpy as np
@@ -7,8 +8,11 @@ import pytest
 import torch
 
 import blocks_reference as ref
+import kv_reference
+import sinks_reference
 from paper_2605_03375_amd import binding as B
 from test_blocks import DEV, NONE, Pool, back, both, gpu, random_pool, words
+from test_kv_ops import make_angles
 
 
 # ---------------------------------------------------------------- entries that name free blocks
@@ -221,3 +225,47 @@ def test_copies_of_more_than_a_grid_takes_at_once(T, h, d, gap, blocks, n):
     B.tutti_blocks_copy(pool, B.make_scales(*scales), d_pairs, words([n]), len(pairs) + len(spare), status)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(planes + scales, want + want_s)) and int(status.item()) == 0
+
+
+# ---------------------------------------------------------------- rotated streams
+
+@gpu
+def test_a_rotated_stream_outlives_its_pool():
+    """200 tokens in a pool of 8 blocks, rotated by their places in the whole stream and not again: results are the definition's over all
+    keys that were ever appended, rotated so; a token beyond the table of angles is refused."""
+    T, h, hq, d, blocks, window, sinks, n = 16, 2, 4, 64, 8, 50, 5, 200
+    rng = np.random.default_rng(4)
+    angles = make_angles(n, d)
+    rope = B.make_rope(torch.from_numpy(angles).to(DEV), d)
+    planes = [torch.zeros(blocks * T * h * d, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    pool = B.make_pool(*planes, num_blocks=blocks, block_tokens=T, num_kv_heads=h, head_dim=d, elt_bytes=2)
+    uses, table = torch.zeros(blocks, dtype=torch.int32, device=DEV), torch.full((16,), -1, dtype=torch.int32, device=DEV)
+    work = torch.empty(B.tutti_blocks_fork_work_bytes(blocks, 1), dtype=torch.uint8, device=DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    x = kv_reference.round16(rng.standard_normal((n + 1, hq + 2 * h, d)), "bf16")
+    # all of it on the CPU: rotated keys and queries, and a cache that holds every block
+    whole = kv_reference.Cache(13, T, h, d, "bf16")
+    want_q, _ = kv_reference.append(whole, "bf16", [(0, n, n, 0)], np.arange(13, dtype=np.uint32), x[:n, :hq], x[:n, hq:hq + h], x[:n, hq + h:],
+                                    dict(cos_sin=angles, rot=d, interleaved=False, pos=None, pairs=None), None)
+    want, _, err, _, _ = sinks_reference.attend(whole, "bf16", [(0, n, n, 0)], np.arange(13, dtype=np.uint32), want_q, hq // h,
+                                                1.0 / math.sqrt(d), window, sinks)
+    for held in range(1, n + 2):
+        if held % T == 1:
+            gone = max(0, held - window) // T
+            B.tutti_blocks_free(uses, blocks, table, 16, words([(1, max(0, gone - 1))]), 1, 16, status)
+            rec = np.zeros(1, B.FORK_DTYPE)
+            rec[0] = (0, held // T, 0, 0, 1, (0, 0, 0))
+            B.tutti_blocks_fork(uses, blocks, table, 16, words(rec.view(np.uint32)), 1, 1, None, None, 0, work, work.numel(), status)
+        row = torch.from_numpy(x[held - 1:held]).to(torch.bfloat16).to(DEV)
+        q, out = torch.full((1, hq, d), math.nan, dtype=torch.bfloat16, device=DEV), torch.empty((1, hq, d), dtype=torch.bfloat16, device=DEV)
+        batch = B.make_batch(words([(0, 1, held, 0)]), 1, 1, table, 16, 1)
+        B.tutti_kv_append(pool, None, batch, rope, B.make_rows(row[:, :hq]), B.make_rows(q), B.make_rows(row[:, hq:hq + h]),
+                          B.make_rows(row[:, hq + h:]), hq, B.BF16, status)
+        if held > n:
+            break
+        attn = B.make_attn(hq, B.BF16, 1.0 / math.sqrt(d), window=window)
+        more = torch.empty(B.tutti_kv_attend_work_bytes(pool, batch, attn), dtype=torch.uint8, device=DEV)
+        B.tutti_kv_attend_sinks(pool, None, batch, attn, sinks, B.make_rows(q), B.make_rows(out), None, more, more.numel(), status)
+        assert np.array_equal(q.float().cpu().numpy()[0], want_q[held - 1])
+        assert (np.abs(out.float().cpu().numpy()[0] - want[held - 1]) <= err[held - 1]).all(), held
+    assert int(status.item()) == B.ST_BAD_POS and bool(torch.isnan(q).all())
