@@ -704,7 +704,7 @@ int tutti_kv_attend_sinks(const tutti_pool *pool, const tutti_scales *scales, co
  * step shares, copies or gives back may be decided on the GPU, and the whole step captured in a graph.  Results are the same from call
  * to call.
  * Common to them: num_blocks below 2^31, max_entries below 2^31 and at most TUTTI_MAX_REQ records (else TUTTI_ERANGE); d_block_table of
- * table_len entries.  Calls on the same counts or tables, and the copies of blocks that they name, go in stream order. */
+ * table_len entries; a block has fewer than 2^31 uses.  Calls on the same counts or tables, and the copies of blocks that they name, go in stream order. */
 #define TUTTI_NO_BLOCK 0xffffffffu /* a table entry, or a pair, that names no block */
 #define TUTTI_ST_NO_FREE 64u   /* tutti_blocks_fork: fewer free blocks than asked for: the entry is TUTTI_NO_BLOCK */
 #define TUTTI_ST_BAD_USES 128u /* a table entry names a block that has no uses.  tutti_blocks_free: its count stays 0.

@@ -236,7 +236,8 @@ __global__ __launch_bounds__(256) void k_blocks_list_free(const ForkArgs a) {
 
 // Uses that a thread adds to (takes from) a block: those of neighbouring records that name the same block at the same place, as samples of
 // one prompt do, go together.  Blocks' counts lie all over memory, and the device makes 27 such additions a nanosecond: 1,024 sequences of
-// 515,000 entries, groups of 8 that share their prompts, 24.4 us one by one, 10.0 so; 384 sequences given back, 32.7 and 11.8.
+// 515,000 entries, groups of 8 that share their prompts, 24.4 us one by one, 10.0 so (and 0.5 for the bits of free blocks, which came
+// later); 384 sequences given back, 32.7 and 11.8.
 struct Run {
   uint32_t id, n;
 };
@@ -274,7 +275,7 @@ __device__ __forceinline__ uint32_t put_entry(const ForkArgs &a, const Fork &f, 
 
 // The second: the same chunk of entries of kGroup neighbouring records to a workgroup.  New block number k lies in the span whose free
 // blocks are numbered around it: a search in LDS over the sums of the spans' counts.
-constexpr uint32_t kGroup = 4;   // (the 1,024 sequences: 4 together 10.0 us, 8 11.5, 16 18.8)
+constexpr uint32_t kGroup = 4;   // (the 1,024 sequences, without the bits: 4 together 10.0 us, 8 11.5, 16 18.8)
 __global__ __launch_bounds__(256) void k_blocks_fork(const ForkArgs a) {
   __shared__ __attribute__((aligned(16))) uint32_t before[kMostSpans];
   __shared__ uint32_t sums[4];
@@ -347,9 +348,12 @@ __global__ __launch_bounds__(256) void k_blocks_fork(const ForkArgs a) {
   if (bad) report(a.status, bad);
 }
 
-// Both in one workgroup, for the few entries of a step in which sequences begin blocks or beams change places: no second launch (4 records
-// of 64 entries, a pool of 65,536 blocks: 5.8 us, the two 7.0 and a pause between them; with the copy in front of it a call of 8.1 and 11.2).
-// Counts are read until there are enough free blocks.  Bound by its trips to memory: records and counts, tables, and what is written.
+// Both in one workgroup, for the few entries of a step in which sequences begin blocks or beams change places: no second launch.  Counts are
+// read until there are enough free blocks, 16,384 at a time, so the pool's size matters where the free ones lie at its end.  4 records of
+// 64 entries, with the copy of the state in front of it, in one launch and in two, us: free blocks everywhere, pools of 32,768 and 65,536
+// blocks 8.4 and 9.9, of 131,072 8.2 and 10.1, of a million 8.4 and 12.2; free blocks at the end alone, 32,768 10.3 and 9.7, 65,536 15.3
+// and 10.2, 131,072 26 and 10.1, a million 170 and 11.8.  So up to 65,536, where a pool that is all but full loses 5 and any other gains
+// 1.6.  Bound by its trips to memory: records and counts, tables, whether the sources' blocks have uses, and what is written.
 constexpr uint32_t kSmallEntries = 4096, kSmallRecords = 1024, kSmallBlocks = 65536;
 __global__ __launch_bounds__(1024) void k_blocks_fork_small(const ForkArgs a) {
   __shared__ Fork records[kSmallRecords];
@@ -604,7 +608,7 @@ __global__ __launch_bounds__(256) void k_blocks_move(const CompactArgs a) {
 #pragma unroll
       for (uint32_t i = 0; i < 4; ++i) {
         if (b[i] >= a.spans.num_blocks && b[i] != kNoBlock) bad |= TUTTI_ST_BAD_BLOCK;
-        // (a block's rank or its word of bits: one load)
+        // a block's rank or its word of bits: one load.  (The words of those in front of the end: 1.2 us of the pass over a million blocks.)
         r[i] = b[i] < a.spans.num_blocks ? a.rank[b[i] >= end ? b[i] : a.used_at + b[i] / 32] : kNoBlock;
       }
 #pragma unroll
@@ -663,7 +667,8 @@ struct CopyArgs {
 constexpr uint32_t kPieceLoads = 4, kPiece = kPieceLoads * kLanes;
 
 // A wavefront copies a piece of 4 KiB of one plane's block; neighbours have neighbouring pieces.  Bound by memory: 6,001 blocks of 32 KiB a
-// plane, 787 MB read and written, in 156 us, 5.0 TB/s (a contiguous copy of 1 GiB by PyTorch: 5.14).
+// plane, 787 MB read and written, in 157 us, 5.0 TB/s (a contiguous copy of 1 GiB by PyTorch: 5.14).  72 registers: seven workgroups a
+// compute unit at once.
 __global__ __launch_bounds__(256) void k_blocks_copy(const CopyArgs a) {
   const uint32_t lane = threadIdx.x & (kLanes - 1);
   const uint32_t n = a.n_pairs ? min(*constant(a.n_pairs), a.max_pairs) : a.max_pairs;

@@ -97,8 +97,13 @@ constexpr uint32_t kUnitTiles = 8;
 // all, the longest `most`.  Lane l weighs parts of (l + 1)/64 of the longest.  A compute unit gets through 0.61 tiles (of 8 heads) a microsecond
 // with one workgroup and 0.72 with more, so that, where row tiles are of one length, time goes by the workgroups of the fullest one of 256
 // compute units, else by all tiles and 0.6 of the last part; in tiles at 0.72, with what a workgroup and a join cost besides.  e4m3, 8 heads,
-// windows of 4,096 keys, us by this rule and by even shares or whole row tiles: 80 sequences of one length 128 and 141, 128 191 and 212, 150
-// 252 and 316; of Zipf lengths 100 125 and 134, 200 248 and 311, 300 353 and 454.  There is work memory for two rounds of slots.
+// windows of 4,096 keys, us by this rule, by even shares and by whole row tiles: 80 sequences of one length 130, 141 and 196, 128 191, 212 and
+// 212, 200 337 by all; of Zipf lengths 100 118, 134 and 193, 200 251, 311 and 311, 300 357, 455 and 455.  It was fitted to these.  Elsewhere, even
+// shares and this: bf16 blocks, 8 heads, Zipf lengths of 300 770 and 603; 8 heads of 64 299 and 235 (200); 5 heads of 80 in e4m3, 300 of one
+// length 476 and 370; 2 heads 286 and 229; windows of 16,000, 300 of Zipf lengths 1,708 and 1,283; windows of 500 within 5 % but for 200 of Zipf
+// lengths, 56.5 and 51.  Of 130 such calls (8, 5, 2 and 1 heads, 80 to 300 sequences) 56 gain more than 8 % and one loses as much: one
+// head, e4m3, 300 of Zipf lengths, 59.4 and 64.5; then bf16, windows of 500, 128 of Zipf lengths, 51.8 and 54.2.  There is work memory for two
+// rounds of slots.
 __device__ __forceinline__ uint32_t parts_of_windows(const AttendArgs &a, uint64_t work, uint64_t rows, uint32_t most) {
   const uint32_t lane = threadIdx.x & (kLanes - 1);
   uint32_t n = static_cast<uint32_t>((static_cast<uint64_t>(most) * (lane + 1) + kLanes - 1) / kLanes);
